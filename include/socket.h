@@ -347,6 +347,90 @@ int socket_decode_step(socket_ctx *ctx, const void *q, const void *K, const void
                        float *scores, int32_t *idx, int32_t *n_selected, int32_t out_dtype,
                        void *out, void *stream);
 
+/*
+ * What a model does to its attention scores and which keys a row sees; NULL wherever one is taken
+ * means nothing of it.  Host memory, read during the call; the arrays it points to are device
+ * memory.  For the row at position i (of a sequence of len tokens) and key j:
+ *     s = softcap tanh(scale q.k / softcap) - slopes[query head] |i - j|
+ * and j is seen when lo(i) <= j <= hi(i), with
+ *     lo(i) = max(0, i - window + 1, doc_begin[b][i]),   hi(i) = min(max(i, prefix_len[b] - 1), len - 1).
+ * Positions are those of the cache as it stands: after an eviction, of the tokens that were kept.
+ */
+typedef struct socket_attn_mods {
+    float softcap;             /* 0: scores are not capped */
+    int32_t window;            /* a row sees itself and the window - 1 keys before it; 0: all of them */
+    const float *slopes;       /* [Hq] bias by distance, or NULL */
+    const int32_t *prefix_len; /* [B] the first tokens that every row sees, or NULL: causal throughout */
+    const int32_t *doc_begin;  /* [B, max_n] the first token of the document that a token belongs to, or NULL */
+} socket_attn_mods;
+
+/*
+ * Eq. 1 for a run of rows per sequence, appended to its cache: one new token, a few, a chunk of a
+ * prompt or all of it.  The caller has written K and V of the run's tokens, positions
+ * row_begin[b] .. row_begin[b] + row_count[b] - 1 of a sequence that is then
+ * row_begin[b] + row_count[b] tokens long (max_rows, on the host, bounds every row_count[b]; a run
+ * that leaves [0, max_n) is cut to it).  For each row i and query head
+ *     out = sum_j softmax(s)_j v_j,   lse = log sum_j exp(s_j)        over the keys the row sees.
+ * q and out: [B, max_rows, Hq, d], out of type out_dtype; lse: float32 [B, max_rows, Hq] or NULL.
+ * Rows behind row_count[b] are left as they were.  A row that sees no key gives zeros and
+ * lse = -inf, and so does one whose scores all are -inf.  Keys and values that a row does not see
+ * never count, infinities and NaN included.  q, K, V and out have to be aligned to 16 bytes.
+ * bf16 caches: fp32 sums; the softmax weights are rounded to bf16 once where out is bf16.
+ * row_begin, row_count: device int32 [batch].
+ */
+int socket_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void *V, const int32_t *block_table,
+                       const int32_t *row_begin, const int32_t *row_count, int32_t batch, int32_t max_rows,
+                       float scale, const socket_attn_mods *mods, int32_t out_dtype, void *out, float *lse,
+                       void *stream);
+
+/*
+ * How much attention each cached key got from a run of rows that socket_attend_rows attended (same
+ * run, scale and mods; lse as it returned it):
+ *     mass[b,h,j] = decay mass[b,h,j] + sum_i sum_g exp(s_ij - lse_i)
+ * over the run's rows i that see j (only the last last_rows of them unless that is 0) and the
+ * query heads g of KV head h.  Tokens of the run itself (j >= row_begin[b]) start from 0, whatever
+ * mass held, and decay = 0 starts all of them from 0; tokens behind the sequence are left as they
+ * were.  Summed in fp32 in a fixed order: the same masses bit for bit on every run.  q and K have
+ * to be aligned to 16 bytes.
+ * mass: device float32 [B, Hkv, max_n] in logical token order, for paged caches too.
+ */
+int socket_key_mass(socket_ctx *ctx, const void *q, const void *K, const float *lse, const int32_t *block_table,
+                    const int32_t *row_begin, const int32_t *row_count, int32_t batch, int32_t max_rows,
+                    float scale, const socket_attn_mods *mods, float decay, int32_t last_rows, float *mass,
+                    void *stream);
+
+/*
+ * Which tokens to keep of a cache: the keep[b] tokens of each (sequence, KV head) with the largest
+ * masses, each taken as the largest of the `pool` masses around it (odd, at most 255; 1: its own),
+ * ties to the smaller position.  The tokens that socket_set_forced_tokens names are always kept
+ * first, and tokens whose block is absent never; a mass that is NaN or -inf ranks below all
+ * others, but its token can be kept, so that every head keeps the same number.  Writes the ranking into
+ * scores ([B, Hkv, max_n] float32, not the array of masses), then idx and n_selected as
+ * socket_topk_select does.  Like that call it discards a pending socket_score_keys_binned.
+ * seq_len, keep: device int32 [batch]; keep[b] is clamped to max_k.
+ */
+int socket_evict_select(socket_ctx *ctx, const float *mass, const int32_t *block_table, const int32_t *seq_len,
+                        const int32_t *keep, int32_t batch, int32_t pool, float *scores, int32_t *idx,
+                        int32_t *n_selected, void *stream);
+
+/*
+ * Evicts: token idx[b,h,j] of each (sequence, KV head) becomes token j, j < n_selected[b,h], of the
+ * _out caches, with its K and V rows and, where they are given, its bucket ids (codes, turned to
+ * the new position), value norm and mass.  The sequence is n_selected tokens long afterwards; rows
+ * behind that are left as they were.  Entries of idx outside [0, max_n), and tokens or new positions whose
+ * block is absent, are skipped.
+ * In place when a cache and its _out are the same tensor under the same block table (give the
+ * same pointer for both); idx then has to ascend strictly, as the selects write it, and paged
+ * sequences must not share blocks.  Otherwise no _out may overlap a source: other tensors, or, paged, blocks
+ * of the same pools that no source sequence uses.  vnorm and mass may be in place in either case.
+ * codes, vnorm and mass: NULL together with their _out.  K, V, codes and their _outs have to be
+ * aligned to 16 bytes.
+ */
+int socket_evict_rows(socket_ctx *ctx, const int32_t *idx, const int32_t *n_selected, int32_t batch,
+                      const void *K, const void *V, const void *codes, const float *vnorm, const float *mass,
+                      const int32_t *block_table, void *K_out, void *V_out, void *codes_out, float *vnorm_out,
+                      float *mass_out, const int32_t *block_table_out, void *stream);
+
 /* Text for an error code; last HIP error code seen by this context (0 if none). */
 const char *socket_strerror(int code);
 int socket_last_hip_error(const socket_ctx *ctx);

@@ -23,6 +23,11 @@ class Params(ctypes.Structure):
         "max_blocks_per_seq", "num_blocks")]
 
 
+class AttnMods(ctypes.Structure):
+    _fields_ = [("softcap", ctypes.c_float), ("window", ctypes.c_int32), ("slopes", ctypes.c_void_p),
+                ("prefix_len", ctypes.c_void_p), ("doc_begin", ctypes.c_void_p)]
+
+
 class SocketError(RuntimeError):
     def __init__(self, code, what):
         self.code = code
@@ -70,6 +75,11 @@ def lib():
         L.socket_dense_decode.argtypes = [vp, vp, vp, vp, vp, vp, i32, f32, i32, vp, vp]
         L.socket_decode_step.argtypes = [vp, vp, vp, vp, vp, vp, f32, vp, vp, vp, vp, i32, f32, vp, vp, vp,
                                          i32, vp, vp]
+        mods = ctypes.POINTER(AttnMods)
+        L.socket_attend_rows.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, f32, mods, i32, vp, vp, vp]
+        L.socket_key_mass.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, f32, mods, f32, i32, vp, vp]
+        L.socket_evict_select.argtypes = [vp, vp, vp, vp, vp, i32, i32, vp, vp, vp, vp]
+        L.socket_evict_rows.argtypes = [vp, vp, vp, i32] + [vp] * 13
         L.socket_strerror.argtypes = [ctypes.c_int]
         L.socket_strerror.restype = ctypes.c_char_p
         L.socket_last_hip_error.argtypes = [vp]
@@ -85,7 +95,7 @@ EXPORTS = ("socket_validate_params", "socket_codes_per_token", "socket_code_posi
            "socket_codes_bytes", "socket_code_location",
            "socket_create", "socket_destroy", "socket_scratch_bytes", "socket_hash_keys",
            "socket_value_norms", "socket_set_forced_tokens",
-           "socket_score", "socket_soft_hash", "socket_hard_hash", "socket_score_keys", "socket_score_keys_binned", "socket_topk_select", "socket_topk_select_binned", "socket_reset", "socket_bucket_probs", "socket_probe_stream_read", "socket_sparse_decode", "socket_sparse_decode_noalloc", "socket_dense_decode", "socket_decode_step", "socket_strerror",
+           "socket_score", "socket_soft_hash", "socket_hard_hash", "socket_score_keys", "socket_score_keys_binned", "socket_topk_select", "socket_topk_select_binned", "socket_reset", "socket_bucket_probs", "socket_probe_stream_read", "socket_sparse_decode", "socket_sparse_decode_noalloc", "socket_dense_decode", "socket_decode_step", "socket_attend_rows", "socket_key_mass", "socket_evict_select", "socket_evict_rows", "socket_strerror",
            "socket_last_hip_error", "socket_graph_begin", "socket_graph_end",
            "socket_graph_launch", "socket_graph_destroy")
 
@@ -148,8 +158,14 @@ def _stream(stream):
     return _raw_stream(_device())
 
 
+def _mods(softcap, window, slopes, prefix_len, doc_begin):
+    if not softcap and not window and slopes is None and prefix_len is None and doc_begin is None:
+        return None
+    return ctypes.byref(AttnMods(float(softcap), int(window), _ptr(slopes), _ptr(prefix_len), _ptr(doc_begin)))
+
+
 class Context:
-    """socket_ctx with the four calls of the decode path as methods."""
+    """socket_ctx with the calls of the path as methods."""
 
     def __init__(self, params: Params):
         self.params = params
@@ -256,6 +272,33 @@ class Context:
                                              _ptr(k), batch, float(scale), _ptr(scores), _ptr(idx),
                                              _ptr(n_selected), out_dtype, _ptr(out), _stream(stream)),
                     "socket_decode_step")
+
+    def attend_rows(self, q, K, V, row_begin, row_count, batch, max_rows, scale, out, lse=None, softcap=0.0, window=0,
+                    slopes=None, prefix_len=None, doc_begin=None, block_table=None, stream=None):
+        out_dtype = F32 if out.dtype == torch.float32 else BF16
+        self._check(lib().socket_attend_rows(self._h, _ptr(q), _ptr(K), _ptr(V), _ptr(block_table), _ptr(row_begin),
+                                             _ptr(row_count), batch, max_rows, float(scale),
+                                             _mods(softcap, window, slopes, prefix_len, doc_begin), out_dtype,
+                                             _ptr(out), _ptr(lse), _stream(stream)), "socket_attend_rows")
+
+    def key_mass(self, q, K, lse, row_begin, row_count, batch, max_rows, scale, mass, decay=1.0, last_rows=0, softcap=0.0,
+                 window=0, slopes=None, prefix_len=None, doc_begin=None, block_table=None, stream=None):
+        self._check(lib().socket_key_mass(self._h, _ptr(q), _ptr(K), _ptr(lse), _ptr(block_table), _ptr(row_begin),
+                                          _ptr(row_count), batch, max_rows, float(scale),
+                                          _mods(softcap, window, slopes, prefix_len, doc_begin), float(decay),
+                                          int(last_rows), _ptr(mass), _stream(stream)), "socket_key_mass")
+
+    def evict_select(self, mass, seq_len, keep, batch, scores, idx, n_selected, pool=1, block_table=None, stream=None):
+        self._check(lib().socket_evict_select(self._h, _ptr(mass), _ptr(block_table), _ptr(seq_len), _ptr(keep), batch,
+                                              int(pool), _ptr(scores), _ptr(idx), _ptr(n_selected), _stream(stream)),
+                    "socket_evict_select")
+
+    def evict_rows(self, idx, n_selected, batch, K, V, K_out, V_out, codes=None, codes_out=None, vnorm=None,
+                   vnorm_out=None, mass=None, mass_out=None, block_table=None, block_table_out=None, stream=None):
+        self._check(lib().socket_evict_rows(self._h, _ptr(idx), _ptr(n_selected), batch, _ptr(K), _ptr(V), _ptr(codes),
+                                            _ptr(vnorm), _ptr(mass), _ptr(block_table), _ptr(K_out), _ptr(V_out),
+                                            _ptr(codes_out), _ptr(vnorm_out), _ptr(mass_out), _ptr(block_table_out),
+                                            _stream(stream)), "socket_evict_rows")
 
 
 def sparse_decode_noalloc(params: Params, q, K, V, idx, n_selected, batch, scale, out, block_table=None,

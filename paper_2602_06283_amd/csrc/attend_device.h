@@ -1,0 +1,164 @@
+// What the attention of a run of rows and the key masses share: which keys a row sees, how a
+// logit comes from its dot product, and the tiles both multiply.
+#pragma once
+
+#include "socket_internal.h"
+
+namespace sk {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// The caller's modifications of the scores, as the kernels take them.  Everything is in units of
+// log 2, so that a weight is one exp2.
+struct RowMods {
+    float c;              // |scale| log2(e) (the queries' signs are turned where scale < 0, which is exact)
+    uint32_t sign;        // 0x80000000 where they are
+    float y_scale, a;     // capped logits: a tanh(y_scale x), a = cap log2(e); a = 0: not capped
+    int general;          // capped, biased or scale = 0: logits are formed before the mask and the maximum
+    int window;
+    const float *slopes;
+    const int32_t *prefix_len;
+    const int32_t *doc_begin;
+};
+
+inline RowMods row_mods(float scale, const socket_attn_mods *m) {
+    RowMods r{};
+    const float s = scale < 0.0f ? -scale : scale;
+    r.sign = scale < 0.0f ? 0x80000000u : 0u;
+    r.c = s * kLog2e;
+    if (m) {
+        if (m->softcap > 0.0f) {
+            r.y_scale = s / m->softcap;
+            r.a = m->softcap * kLog2e;
+        }
+        r.window = m->window;
+        r.slopes = m->slopes;
+        r.prefix_len = m->prefix_len;
+        r.doc_begin = m->doc_begin;
+    }
+    r.general = r.a > 0.0f || r.slopes != nullptr || r.c == 0.0f;
+    return r;
+}
+
+// A run of rows: token positions begin .. begin + count - 1 of a sequence that is begin + count
+// long.  One that leaves [0, max_n) is cut to it.
+struct RowRun {
+    int begin, count;
+    __device__ __forceinline__ RowRun(const int32_t *row_begin, const int32_t *row_count, int b, int max_rows, int max_n) {
+        begin = scalar_load(&row_begin[b]);
+        count = min(scalar_load(&row_count[b]), max_rows);
+        if (begin < 0 || begin >= max_n) begin = count = 0;
+        count = max(0, min(count, max_n - begin));
+    }
+    __device__ __forceinline__ int len() const { return begin + count; }
+};
+
+// keys lo .. hi that the row at position i sees (none where lo > hi)
+__device__ __forceinline__ void row_span(const RowMods &m, int b, int i, int len, int max_n, int &lo, int &hi) {
+    lo = 0;
+    hi = i;
+    if (m.window > 0) lo = max(lo, i - m.window + 1);
+    if (m.doc_begin) lo = max(lo, m.doc_begin[(int64_t)b * max_n + i]);
+    if (m.prefix_len) {
+        const int p = m.prefix_len[b];
+        if (p > i) hi = p - 1;
+    }
+    hi = min(hi, len - 1);
+}
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// tanh to about four units in the last place: its power series up to |y| = 1/4 (the first term left
+// out, 1382/155925 y^11, is 8e-9 of it there), beyond that 1 - 2 / (1 + e^2y), whose rounding is
+// absolute and would be felt only near zero.
+__device__ __forceinline__ float tanh_series(float y) {
+    const float z = y * y;
+    const float t = fmaf(fmaf(fmaf(fmaf(62.0f / 2835.0f, z, -17.0f / 315.0f), z, 2.0f / 15.0f), z, -1.0f / 3.0f), z, 1.0f);
+    return y * t;
+}
+__device__ __forceinline__ float tanh_any(float y) {
+    const float far = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + exp2_fast(y * (2.0f * kLog2e))), 1.0f);
+    return fabsf(y) <= 0.25f ? tanh_series(y) : far;
+}
+
+// the logit (in units of log 2) of a dot product, at distance dist = i - j, slope2 = slope log2(e)
+__device__ __forceinline__ float logit2(const RowMods &m, float x, float dist, float slope2) {
+    float s = m.a > 0.0f ? m.a * tanh_any(x * m.y_scale) : x * m.c;
+    if (m.slopes) s = fmaf(-slope2, fabsf(dist), s);
+    return s;
+}
+
+// The same for the N dot products of one query that a lane holds of a tile, key of x[n] = key0 +
+// row_of(n): capped logits are mostly far below the cap, so a wavefront whose arguments all are
+// small takes the series alone.
+template <int N, typename F>
+__device__ __forceinline__ void logits2(const RowMods &m, float (&x)[N], float i_minus_key0, float slope2, F row_of) {
+    if (m.a > 0.0f) {
+        float top = 0.0f;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            x[n] *= m.y_scale;
+            top = fmaxf(top, fabsf(x[n]));
+        }
+        if (__all(top <= 0.25f)) {
+#pragma unroll
+            for (int n = 0; n < N; ++n) x[n] = m.a * tanh_series(x[n]);
+        } else {
+#pragma unroll
+            for (int n = 0; n < N; ++n) x[n] = m.a * tanh_any(x[n]);
+        }
+    } else {
+#pragma unroll
+        for (int n = 0; n < N; ++n) x[n] *= m.c;
+    }
+    if (m.slopes) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) x[n] = fmaf(-slope2, fabsf(i_minus_key0 - (float)row_of(n)), x[n]);
+    }
+}
+
+// ---- matrix tiles: 32 keys x 32 queries, logits as K Q^T, so that a lane holds one query's
+// logits and the softmax runs along its registers
+typedef float floatx16_t __attribute__((ext_vector_type(16)));
+typedef __attribute__((__vector_size__(8 * sizeof(__bf16)))) __bf16 bf16x8v_t;
+
+// key row of accumulator register r in a 32 x 32 tile, for lane half hf
+__device__ __forceinline__ constexpr int tile_row(int r, int hf) { return 8 * (r / 4) + 4 * hf + r % 4; }
+
+// One 16-byte piece of a row in the operand layouts used here.  bf16: 8 channels, one k-step of 16
+// takes piece 2 ks + hf.  fp32: 4 channels, two-channel k-steps 4 c .. 4 c + 3 take piece 2 c + hf
+// (which channels meet in a step is free as long as both operands agree).
+template <typename T> __device__ __forceinline__ void mma_piece(floatx16_t &c, u32x4_t a, u32x4_t b);
+template <> __device__ __forceinline__ void mma_piece<uint16_t>(floatx16_t &c, u32x4_t a, u32x4_t b) {
+    c = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8v_t, a), __builtin_bit_cast(bf16x8v_t, b), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ void mma_piece<float>(floatx16_t &c, u32x4_t a, u32x4_t b) {
+    const f32x4_t x = __builtin_bit_cast(f32x4_t, a), y = __builtin_bit_cast(f32x4_t, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], c, 0, 0, 0);
+}
+
+// turns the sign of a piece's channels
+template <typename T> __device__ __forceinline__ u32x4_t turn_sign(u32x4_t v, uint32_t sign) {
+    const uint32_t s = sizeof(T) == 2 ? sign | (sign >> 16) : sign;
+    return v ^ s;
+}
+
+// sizes and swizzles of the K / V tiles in LDS, in pieces of 16 bytes
+template <typename T, int D> struct KvTile {
+    static constexpr int KT = sizeof(T) == 2 ? 64 : 32;          // keys
+    static constexpr int ROWB = D * (int)sizeof(T);
+    static constexpr int CPR = ROWB / 16;                        // pieces per row
+    static constexpr int BYTES = KT * ROWB;
+    // K: 32 rows are read at one piece each: the piece is turned by the row
+    static __device__ __forceinline__ int k_piece(int row, int c) { return row * CPR + (c ^ (row & (CPR < 16 ? CPR - 1 : 15))); }
+    // V: bf16 rows are read four at a time, 64 bytes each, and transposed on the way; fp32 rows r and
+    // r + 4 at once, 128 bytes each
+    static __device__ __forceinline__ int v_turn(int row) {
+        if (sizeof(T) == 4) return ((row >> 2) & 1) << 3;
+        return CPR == 8 ? ((row >> 1) & 1) << 2 : (row & 3) << 2;
+    }
+    static __device__ __forceinline__ int v_piece(int row, int c) { return row * CPR + (c ^ v_turn(row)); }
+};
+
+}  // namespace sk

@@ -1,0 +1,533 @@
+// Attention of a run of query rows per sequence over its cache: one new token, a few, a chunk of
+// a prompt or a whole one.  Row at position i, query head g, keys j it sees (row_span):
+//     s_j = cap tanh(scale q.k_j / cap) - slope |i - j|,   out = sum_j softmax(s)_j v_j,   lse = log sum_j exp(s_j)
+//
+// One pass over the keys with a running maximum and sum.  The G query heads of a KV head and the
+// rows of the run are one axis of queries, m = row * G + g; a workgroup takes 128 of them, 32 per
+// wavefront, and all of its wavefronts walk the same tiles of keys through LDS.  A wavefront forms
+// K Q^T (32 keys x 32 queries a tile), so that a lane holds logits of one query and the softmax
+// needs one exchange between the lane halves; the weights, as they lie in the accumulators, are
+// the B operand of V^T P^T once V's rows are taken in the same order (rows 0-3 and 8-11 of 16 for
+// the lower lanes, 4-7 and 12-15 for the upper), so they never leave their lanes.
+//
+// bf16 caches: products of bf16 with fp32 sums.  The weights are rounded once to bf16 where the
+// output is bf16 (half a step each, as the output's own rounding); where the output is fp32 they
+// go in as three bf16 pieces, which hold all 24 bits.  fp32 caches: fp32 matrix instructions.
+//
+// Few rows: the keys are split over workgroups, whose (maximum, sum, weighted values) a second
+// launch joins, split by split in a fixed order.
+//
+// Values at masked keys never count, whatever they are: a masked weight is 0, but 0 times an
+// infinity is not, so a wavefront that ends with a value that is not finite goes over its row
+// again one key at a time (attend_plain).
+#include "attend_device.h"
+
+namespace sk {
+
+constexpr int kRowsThreads = 256;
+constexpr int kRowsQueries = 128;                // queries per workgroup
+
+struct RowsArgs {
+    const void *q;
+    const void *K;
+    const void *V;
+    void *out;
+    float *lse;
+    float *partials;
+    const int32_t *row_begin;
+    const int32_t *row_count;
+    RowMap map;
+    RowMods mods;
+    int BH, Hq, G, g_log2, max_rows, n_tiles, n_split, out_dtype;
+};
+
+// where a query's result goes: its index among all (sequence, row, query head)
+__device__ __forceinline__ int64_t query_at(const RowsArgs &a, int b, int h, int m) {
+    return ((int64_t)b * a.max_rows + (m >> a.g_log2)) * a.Hq + h * a.G + (m & (a.G - 1));
+}
+
+// One query over keys j0 .. j1 by a whole wavefront, key by key: lane = key for the logits, lane =
+// channels for the values.  Only for rows that meet infinities or NaN.
+template <typename T, int D>
+__device__ __forceinline__ void attend_plain(const RowsArgs &a, int b, int h, int m, int i, int j0, int j1, int split) {
+    constexpr int PER = D / 64;
+    const int lane = threadIdx.x & 63;
+    const int64_t at = query_at(a, b, h, m);
+    const T *q = (const T *)a.q + at * D;
+    const float slope2 = a.mods.slopes ? a.mods.slopes[h * a.G + (m & (a.G - 1))] * kLog2e : 0.0f;
+    const float ninf = -__builtin_inff();
+    float top = ninf, sum = 0.0f, acc[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) acc[k] = 0.0f;
+    for (int j = j0; j <= j1; j += 64) {
+        const int t = j + lane;
+        const int64_t row = t <= j1 ? a.map.row(b, h, t) : -1;
+        float s = ninf;
+        if (row >= 0) {
+            float dot = 0.0f;
+#pragma clang loop unroll(disable)
+            for (int c = 0; c < D; c += 8) {
+                Row8<T> kr, qr;
+                kr.load((const T *)a.K + row * D + c);
+                qr.load(q + c);
+                float kf[8], qf[8];
+                kr.get(kf);
+                qr.get(qf);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) dot = fmaf(kf[e], __uint_as_float(__float_as_uint(qf[e]) ^ a.mods.sign), dot);
+            }
+            s = logit2(a.mods, dot, (float)(i - t), slope2);
+        }
+        const float top_new = fmaxf(top, wave_max(s)), use = top_new == ninf ? 0.0f : top_new;
+        const float p = row >= 0 ? exp2_fast(s - use) : 0.0f, alpha = exp2_fast(top - use);
+        top = top_new;
+        sum = sum * alpha + p;
+#pragma unroll
+        for (int k = 0; k < PER; ++k) acc[k] *= alpha;
+        const unsigned long long there = __ballot(row >= 0);
+#pragma clang loop unroll(disable)
+        for (int o = 0; o < 64; ++o) {
+            if (!((there >> o) & 1ull)) continue;
+            const float w = __shfl(p, o);
+            const int64_t vrow = a.map.row(b, h, j + o);
+#pragma unroll
+            for (int k = 0; k < PER; ++k) {
+                const T *v = (const T *)a.V + vrow * D + lane + 64 * k;
+                const float x = sizeof(T) == 2 ? bf16_to_f32(*(const uint16_t *)v) : *(const float *)v;
+                acc[k] = fmaf(w, x, acc[k]);
+            }
+        }
+    }
+    sum = row_sum<64>(sum);
+    if (a.n_split > 1) {
+        float *part = a.partials + (at * a.n_split + split) * (D + 2);
+        if (lane == 0) {
+            part[0] = top;
+            part[1] = sum;
+        }
+#pragma unroll
+        for (int k = 0; k < PER; ++k) part[2 + lane + 64 * k] = acc[k];
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const float y = sum == 0.0f ? 0.0f : acc[k] / sum;
+        if (a.out_dtype == SOCKET_F32) ((float *)a.out)[at * D + lane + 64 * k] = y;
+        else ((uint16_t *)a.out)[at * D + lane + 64 * k] = f32_to_bf16_rne(y);
+    }
+    if (a.lse && lane == 0) a.lse[at] = sum == 0.0f ? ninf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+typedef short shortx4_t __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) shortx4_t lds_shortx4_t;
+
+// two floats rounded to bf16, to nearest even (one instruction)
+typedef float floatx2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2_t{lo, hi}, bf16x2_t));
+}
+
+// O^T += V^T P^T over the 32 keys of sub-tile u; p: the weights as the logits' tile left them
+template <typename T, int D, int PX> struct ValueProduct;
+template <int D, int PX> struct ValueProduct<uint16_t, D, PX> {
+    static __device__ __forceinline__ void run(floatx16_t (&o)[D / 32], const char *v, int u, float (&p)[16], int lane) {
+        using Tile = KvTile<uint16_t, D>;
+        const int hf = lane >> 5;
+#pragma unroll
+        for (int ks = 0; ks < 2; ++ks) {
+            u32x4_t w[PX];
+#pragma unroll
+            for (int x = 0; x < PX; ++x) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float &p0 = p[8 * ks + 2 * e], &p1 = p[8 * ks + 2 * e + 1];
+                    w[x][e] = pack_bf16(p0, p1);
+                    if (x + 1 < PX) {
+                        p0 -= __uint_as_float(w[x][e] << 16);
+                        p1 -= __uint_as_float(w[x][e] & 0xffff0000u);
+                    }
+                }
+            }
+            // rows 16 ks + 4 hf + 0..3 and + 8: the lane's sixteenth of the wavefront reads four rows of
+            // 16 channels, transposed
+            const int row = 32 * u + 16 * ks + 4 * hf + ((lane & 15) >> 2);
+            const int c0 = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), in = (lane & 1) * 8;
+#pragma unroll
+            for (int cb = 0; cb < D / 32; ++cb) {
+                union { shortx4_t h[2]; u32x4_t v; } f;
+                f.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(v + Tile::v_piece(row, c0 + 4 * cb) * 16 + in));
+                f.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(v + Tile::v_piece(row + 8, c0 + 4 * cb) * 16 + in));
+#pragma unroll
+                for (int x = 0; x < PX; ++x) mma_piece<uint16_t>(o[cb], f.v, w[x]);
+            }
+        }
+    }
+};
+template <int D, int PX> struct ValueProduct<float, D, PX> {
+    static __device__ __forceinline__ void run(floatx16_t (&o)[D / 32], const char *v, int u, float (&p)[16], int lane) {
+        using Tile = KvTile<float, D>;
+        const int hf = lane >> 5, ch = lane & 31;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            const int row = 32 * u + tile_row(r, hf);
+#pragma unroll
+            for (int cb = 0; cb < D / 32; ++cb) {
+                const float x = *(const float *)(v + Tile::v_piece(row, 8 * cb + (ch >> 2)) * 16 + (ch & 3) * 4);
+                o[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[r], o[cb], 0, 0, 0);
+            }
+        }
+    }
+};
+
+template <typename T, int D> constexpr size_t rows_lds() { return (size_t)4 * KvTile<T, D>::BYTES; }
+
+template <typename T, int D, int PX>
+__global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_kernel(RowsArgs a) {
+    using Tile = KvTile<T, D>;
+    constexpr int KT = Tile::KT, CPR = Tile::CPR, NU = KT / 32, NG = KT / 16;
+    constexpr int LOADS = KT * CPR / kRowsThreads;               // pieces of K (and of V) a thread brings
+    constexpr int NKS = CPR / 2;                                 // pairs of pieces along the channels
+    extern __shared__ __align__(16) char rows_tiles[];           // [2][K tile, V tile]
+    __shared__ int s_lo[4], s_hi[4];
+    __shared__ __align__(16) int s_absent[2][4];                 // sixteenths of a tile whose block is absent
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hf = lane >> 5;
+    // all workgroups of a KV head on one XCD where there are eight heads or more (its L2 then serves the
+    // head's keys), long rows first
+    const int bh = (int)blockIdx.x % a.BH, rest = (int)blockIdx.x / a.BH;
+    const int split = rest % a.n_split, qt = a.n_tiles - 1 - rest / a.n_split;
+    const int b = bh / a.map.Hkv, h = bh - b * a.map.Hkv;
+    const RowRun run(a.row_begin, a.row_count, b, a.max_rows, a.map.max_n);
+    if (qt * kRowsQueries >= run.count * a.G) return;
+
+    // ---- this lane's query: the two halves of the wavefront share it
+    const int m = qt * kRowsQueries + wave * 32 + (lane & 31);
+    const bool valid = (m >> a.g_log2) < run.count;
+    const int i = run.begin + (m >> a.g_log2);
+    int lo = 0, hi = -1;
+    u32x4_t q[NKS];
+    if (valid) {
+        row_span(a.mods, b, i, run.len(), a.map.max_n, lo, hi);
+        const T *src = (const T *)a.q + query_at(a, b, h, m) * D;
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) q[ks] = turn_sign<T>(*(const u32x4_t *)((const char *)src + (2 * ks + hf) * 16), a.mods.sign);
+    } else {
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) q[ks] = 0;
+    }
+    const float slope2 = a.mods.slopes && valid ? a.mods.slopes[h * a.G + (m & (a.G - 1))] * kLog2e : 0.0f;
+
+    // ---- the keys any query of the workgroup sees
+    const bool sees = lo <= hi;
+    int lo_w = sees ? lo : 0x7fffffff, hi_w = sees ? hi : -1;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        lo_w = min(lo_w, __shfl_xor(lo_w, o));
+        hi_w = max(hi_w, __shfl_xor(hi_w, o));
+    }
+    if (lane == 0) {
+        s_lo[wave] = lo_w;
+        s_hi[wave] = hi_w;
+    }
+    __syncthreads();
+    const int k_lo = min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3]));
+    const int k_hi = __builtin_amdgcn_readfirstlane(max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3])));
+    const int base = __builtin_amdgcn_readfirstlane(k_lo & ~15);
+    const int n_tiles = k_hi >= 0 ? (k_hi - base) / KT + 1 : 0;
+    const int per = (n_tiles + a.n_split - 1) / a.n_split;
+    const int t_begin = split * per, t_end = min(n_tiles, t_begin + per);
+
+    // ---- staging: 16-byte pieces of 64 / CPR rows per wavefront and load, all of them in one sixteenth
+    //      of the cache (a block holds whole ones), so the block is one scalar look-up
+    u32x4_t kreg[LOADS], vreg[LOADS];
+    bool absent[LOADS];
+    auto load = [&](int tile) __attribute__((always_inline)) {
+#pragma unroll
+        for (int p = 0; p < LOADS; ++p) {
+            const int id = p * kRowsThreads + tid, row = id / CPR, c = id % CPR;
+            const int t = min(base + tile * KT + row, k_hi);
+            int64_t at;
+            absent[p] = false;
+            if (a.map.block_table == nullptr) {
+                at = (int64_t)bh * a.map.max_n + t;
+            } else {
+                const int slot = a.map.page_slot(__builtin_amdgcn_readfirstlane(t));
+                int blk = scalar_load(&a.map.block_table[(int64_t)b * a.map.max_blocks + slot]);
+                absent[p] = (unsigned)blk >= (unsigned)a.map.num_blocks;
+                if (absent[p]) blk = 0;
+                at = ((int64_t)blk * a.map.Hkv + h) * a.map.page + (t - slot * a.map.page);
+            }
+            kreg[p] = *(const u32x4_t *)((const char *)a.K + at * Tile::ROWB + c * 16);
+            vreg[p] = *(const u32x4_t *)((const char *)a.V + at * Tile::ROWB + c * 16);
+        }
+    };
+    auto store = [&](int buf) __attribute__((always_inline)) {
+        char *kt = rows_tiles + buf * 2 * Tile::BYTES, *vt = kt + Tile::BYTES;
+#pragma unroll
+        for (int p = 0; p < LOADS; ++p) {
+            const int id = p * kRowsThreads + tid, row = id / CPR, c = id % CPR;
+            *(u32x4_t *)(kt + Tile::k_piece(row, c) * 16) = kreg[p];
+            *(u32x4_t *)(vt + Tile::v_piece(row, c) * 16) = vreg[p];
+            if (c == 0 && (row & 15) == 0) s_absent[buf][row >> 4] = absent[p];
+        }
+    };
+
+    floatx16_t o[D / 32];
+#pragma unroll
+    for (int cb = 0; cb < D / 32; ++cb) o[cb] = 0.0f;
+    const float ninf = -__builtin_inff();
+    float top = ninf, sum = 0.0f;                    // running maximum and this lane's half of the running sum
+    if (t_begin < t_end) {
+        load(t_begin);
+        store(0);
+    }
+    __syncthreads();
+    for (int tile = t_begin; tile < t_end; ++tile) {
+        const int buf = (tile - t_begin) & 1;
+        const char *kt = rows_tiles + buf * 2 * Tile::BYTES, *vt = kt + Tile::BYTES;
+        const bool more = tile + 1 < t_end;
+        if (more) load(tile + 1);
+        const int t0 = base + tile * KT;
+        if (__any(valid && lo <= t0 + KT - 1 && hi >= t0)) {
+            // ---- logits
+            float s[NU][16];
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                floatx16_t c = 0.0f;
+                const int row = 32 * u + (lane & 31);
+#pragma unroll
+                for (int ks = 0; ks < NKS; ++ks)
+                    mma_piece<T>(c, *(const u32x4_t *)(kt + Tile::k_piece(row, 2 * ks + hf) * 16), q[ks]);
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[u][r] = c[r];
+            }
+            float cc = a.mods.c;
+            if (a.mods.general) {
+#pragma unroll
+                for (int u = 0; u < NU; ++u)
+                    logits2(a.mods, s[u], (float)(i - t0 - 32 * u), slope2, [&](int r) { return tile_row(r, hf); });
+                cc = 1.0f;
+            }
+            // ---- masks
+            int gone = 0;
+            if (a.map.block_table) {
+#pragma unroll
+                for (int g = 0; g < NG; ++g) gone |= s_absent[buf][g] << g;
+                gone = __builtin_amdgcn_readfirstlane(gone);
+            }
+            if (__any(valid && (lo > t0 || hi < t0 + KT - 1)) || gone) {
+                const uint32_t span = (uint32_t)(hi - lo);
+                const bool any = lo <= hi;
+#pragma unroll
+                for (int u = 0; u < NU; ++u) {
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        const int row = 32 * u + tile_row(r, hf);
+                        const bool vis = any && (uint32_t)(t0 + row - lo) <= span && !((gone >> (2 * u + r / 8)) & 1);
+                        s[u][r] = vis ? s[u][r] : ninf;
+                    }
+                }
+            }
+            // ---- running maximum, weights and their sum
+            float mx = s[0][0];
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[u][r]);
+            {
+                auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+                mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+            }
+            const float top_new = fmaxf(top, mx == ninf ? ninf : mx * cc);
+            const float use = top_new == ninf ? 0.0f : top_new;
+            if (__any(top_new > top)) {
+                const float alpha = exp2_fast(top - use);
+                sum *= alpha;
+#pragma unroll
+                for (int cb = 0; cb < D / 32; ++cb) o[cb] *= alpha;
+            }
+            top = top_new;
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                float part = 0.0f;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    s[u][r] = exp2_fast(fmaf(s[u][r], cc, -use));
+                    part += s[u][r];
+                }
+                sum += part;
+            }
+            // ---- values
+#pragma unroll
+            for (int u = 0; u < NU; ++u) ValueProduct<T, D, PX>::run(o, vt, u, s[u], lane);
+        }
+        if (more) store(buf ^ 1);
+        __syncthreads();
+    }
+
+    // ---- results
+    sum = xor32_sum(sum);
+    float check = 0.0f * sum;
+#pragma unroll
+    for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) check = fmaf(0.0f, o[cb][r], check);
+    unsigned long long again = __ballot(valid && !(check == 0.0f));
+    again = (again | (again >> 32)) & 0xffffffffull;
+    if (valid && !((again >> (lane & 31)) & 1ull)) {
+        const int64_t at = query_at(a, b, h, m);
+        if (a.n_split > 1) {
+            float *part = a.partials + (at * a.n_split + split) * (D + 2);
+            if (hf == 0) *(float2 *)part = make_float2(top, sum);
+#pragma unroll
+            for (int cb = 0; cb < D / 32; ++cb)
+#pragma unroll
+                for (int r = 0; r < 16; r += 2) *(float2 *)(part + 2 + 32 * cb + tile_row(r, hf)) = make_float2(o[cb][r], o[cb][r + 1]);
+        } else {
+            const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+            for (int cb = 0; cb < D / 32; ++cb) {
+#pragma unroll
+                for (int r = 0; r < 16; r += 4) {
+                    const int ch = 32 * cb + tile_row(r, hf);
+                    const f32x4_t y = {o[cb][r] * inv, o[cb][r + 1] * inv, o[cb][r + 2] * inv, o[cb][r + 3] * inv};
+                    if (a.out_dtype == SOCKET_F32) *(f32x4_t *)((float *)a.out + at * D + ch) = y;
+                    else *(uint2 *)((uint16_t *)a.out + at * D + ch) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+                }
+            }
+            if (a.lse && hf == 0) a.lse[at] = sum == 0.0f ? ninf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+        }
+    }
+    while (again) {
+        const int n = __builtin_ctzll(again);
+        again &= again - 1;
+        const int nlo = max(__builtin_amdgcn_readlane(lo, n), base + t_begin * KT);
+        const int nhi = min(__builtin_amdgcn_readlane(hi, n), base + t_end * KT - 1);
+        attend_plain<T, D>(a, b, h, __builtin_amdgcn_readlane(m, n), __builtin_amdgcn_readlane(i, n), nlo, nhi, split);
+    }
+}
+
+// Joins the splits of one query: out = sum_s w_s acc_s / sum_s w_s l_s, w_s = exp2(m_s - max m).
+constexpr int kRowsMergeThreads = 256;
+template <int D>
+__global__ __launch_bounds__(kRowsMergeThreads) void attend_rows_merge_kernel(RowsArgs a) {
+    constexpr int NG = kRowsMergeThreads / D;
+    __shared__ float s_w[kMaxSplits], s_red[kRowsMergeThreads], s_sum, s_top;
+    const int tid = threadIdx.x, c = tid % D, grp = tid / D;
+    const int hq = blockIdx.x, r = blockIdx.y, b = blockIdx.z;
+    const RowRun run(a.row_begin, a.row_count, b, a.max_rows, a.map.max_n);
+    if (r >= run.count) return;
+    const int64_t at = ((int64_t)b * a.max_rows + r) * a.Hq + hq;
+    const float *part = a.partials + at * a.n_split * (D + 2);
+    const float ninf = -__builtin_inff();
+    if (tid < 64) {
+        float m[2], l[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int s = tid + 64 * j;
+            m[j] = s < a.n_split ? part[(int64_t)s * (D + 2)] : ninf;
+            l[j] = s < a.n_split ? part[(int64_t)s * (D + 2) + 1] : 0.0f;
+        }
+        const float top = wave_max(fmaxf(m[0], m[1])), use = top == ninf ? 0.0f : top;
+        const float w0 = exp2_fast(m[0] - use), w1 = exp2_fast(m[1] - use);
+        const float sum = row_sum<64>(w0 * l[0] + w1 * l[1]);
+        s_w[tid] = w0;
+        s_w[tid + 64] = w1;
+        if (tid == 0) {
+            s_sum = sum;
+            s_top = top;
+        }
+    }
+    __syncthreads();
+    float acc = 0.0f;
+    for (int s = grp; s < a.n_split; s += NG) {
+        const float w = s_w[s];
+        const float x = part[(int64_t)s * (D + 2) + 2 + c];
+        if (w > 0.0f || w != w) acc = fmaf(w, x, acc);           // (an empty split's values are zeros)
+    }
+    s_red[tid] = acc;
+    __syncthreads();
+    if (grp == 0) {
+#pragma unroll
+        for (int k = 1; k < NG; ++k) acc += s_red[k * D + c];
+        const float sum = s_sum, y = sum == 0.0f ? 0.0f : acc / sum;
+        if (a.out_dtype == SOCKET_F32) ((float *)a.out)[at * D + c] = y;
+        else ((uint16_t *)a.out)[at * D + c] = f32_to_bf16_rne(y);
+        if (a.lse && c == 0) a.lse[at] = sum == 0.0f ? ninf : (s_top + __builtin_amdgcn_logf(sum)) * kLn2;
+    }
+}
+
+template <typename T, int D> static int rows_allow() {
+    constexpr size_t lds = rows_lds<T, D>();
+    if (lds <= 64 * 1024) return SOCKET_OK;
+    auto allow = [](auto kernel) {
+        return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess;
+    };
+    bool ok = allow(attend_rows_kernel<T, D, 1>);
+    if constexpr (sizeof(T) == 2) ok = ok && allow(attend_rows_kernel<T, D, 3>);
+    return ok ? SOCKET_OK : SOCKET_EHIP;
+}
+
+int attend_prepare(int d, int kv_dtype) {
+    const bool f32 = kv_dtype == SOCKET_F32;
+    return d == 64    ? (f32 ? rows_allow<float, 64>() : rows_allow<uint16_t, 64>())
+           : d == 128 ? (f32 ? rows_allow<float, 128>() : rows_allow<uint16_t, 128>())
+                      : (f32 ? rows_allow<float, 256>() : rows_allow<uint16_t, 256>());
+}
+
+template <typename T, int D> static void launch_rows(const RowsArgs &a, dim3 grid, hipStream_t st) {
+    constexpr size_t lds = rows_lds<T, D>();
+    if constexpr (sizeof(T) == 2) {
+        if (a.out_dtype == SOCKET_F32) {
+            hipLaunchKernelGGL((attend_rows_kernel<T, D, 3>), grid, dim3(kRowsThreads), lds, st, a);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((attend_rows_kernel<T, D, 1>), grid, dim3(kRowsThreads), lds, st, a);
+}
+
+int launch_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void *V, const int32_t *block_table,
+                       const int32_t *row_begin, const int32_t *row_count, int batch, int max_rows, float scale,
+                       const socket_attn_mods *mods, int out_dtype, void *out, float *lse, hipStream_t st) {
+    const Geometry &g = ctx->g;
+    RowsArgs a;
+    a.q = q; a.K = K; a.V = V; a.out = out; a.lse = lse; a.partials = ctx->partials;
+    a.row_begin = row_begin; a.row_count = row_count;
+    a.map = row_map(g, block_table);
+    a.mods = row_mods(scale, mods);
+    a.BH = batch * g.Hkv; a.Hq = g.Hq; a.G = g.G; a.g_log2 = __builtin_ctz((unsigned)g.G);
+    a.max_rows = max_rows; a.out_dtype = out_dtype;
+    a.n_tiles = (int)(((int64_t)max_rows * g.G + kRowsQueries - 1) / kRowsQueries);
+    // Two workgroups per compute unit keep it busy; with fewer the keys are split, down to four tiles each
+    // and as far as the partial results fit.
+    const int64_t wgs = (int64_t)a.BH * a.n_tiles;
+    const int64_t room = ctx->partial_floats / ((int64_t)batch * max_rows * g.Hq * (g.d + 2));
+    int64_t n = 512 / wgs;
+    const int64_t most = (g.max_n + 255) / 256;
+    n = n < most ? n : most;
+    n = n < room ? n : room;
+    n = n < kMaxSplits ? n : kMaxSplits;
+    a.n_split = n < 1 ? 1 : (int)n;
+    const int64_t grid = wgs * a.n_split;
+    if (grid >= (int64_t)1 << 31) return SOCKET_EUNSUPPORTED;
+    const bool f32 = g.kv_dtype == SOCKET_F32;
+    const dim3 gr((unsigned)grid);
+    switch (g.d) {
+        case 64: f32 ? launch_rows<float, 64>(a, gr, st) : launch_rows<uint16_t, 64>(a, gr, st); break;
+        case 128: f32 ? launch_rows<float, 128>(a, gr, st) : launch_rows<uint16_t, 128>(a, gr, st); break;
+        case 256: f32 ? launch_rows<float, 256>(a, gr, st) : launch_rows<uint16_t, 256>(a, gr, st); break;
+        default: return SOCKET_EUNSUPPORTED;
+    }
+    if (a.n_split > 1) {
+        const dim3 mg(g.Hq, max_rows, batch);
+        switch (g.d) {
+            case 64: hipLaunchKernelGGL(attend_rows_merge_kernel<64>, mg, dim3(kRowsMergeThreads), 0, st, a); break;
+            case 128: hipLaunchKernelGGL(attend_rows_merge_kernel<128>, mg, dim3(kRowsMergeThreads), 0, st, a); break;
+            default: hipLaunchKernelGGL(attend_rows_merge_kernel<256>, mg, dim3(kRowsMergeThreads), 0, st, a); break;
+        }
+    }
+    return record_hip(ctx, hipGetLastError());
+}
+
+}  // namespace sk

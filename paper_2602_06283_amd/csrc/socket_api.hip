@@ -1,4 +1,6 @@
 // C-ABI entry points of libsocket: parameter checks, scratch ownership, dispatch.
+#include <algorithm>
+#include <initializer_list>
 #include <new>
 
 #include "socket_internal.h"
@@ -205,9 +207,13 @@ int socket_create(socket_ctx **out, const socket_params *p) {
     const int64_t sz_staged = BH * g.max_k * 4;
     const int64_t sz_regions = BH * g.n_regions * kSlice * 4, sz_selcnt = BH * g.n_regions * 4;
     const int64_t sz_seq = (int64_t)g.max_batch * 4;
-    const int64_t sz_part = (int64_t)g.max_batch * g.Hq * kMaxSplits * (g.d + 2) * 4;
+    // (runs of rows split their keys as far as this holds the partial results: 32 MiB are 31 splits of 64
+    // rows of 32 query heads, d = 128)
+    const int64_t sz_part = std::max((int64_t)g.max_batch * g.Hq * kMaxSplits * (g.d + 2) * 4, (int64_t)32 << 20);
+    ctx->partial_floats = sz_part / 4;
     ctx->scratch_bytes = sz_tables + sz_tstats + sz_sub + sz_hist + sz_cnt + 2 * sz_cand + sz_staged + sz_regions + sz_selcnt + sz_part + sz_seq;
-    bool ok = score_prepare(g) == SOCKET_OK &&
+    bool ok = score_prepare(g) == SOCKET_OK && attend_prepare(g.d, g.kv_dtype) == SOCKET_OK &&
+              mass_prepare(g.d, g.kv_dtype) == SOCKET_OK &&
               hipMalloc((void **)&ctx->tables, sz_tables) == hipSuccess &&
               hipMalloc((void **)&ctx->tstats, sz_tstats) == hipSuccess &&
               (sz_sub == 0 || hipMalloc((void **)&ctx->subprobs, sz_sub) == hipSuccess) &&
@@ -382,6 +388,71 @@ int socket_dense_decode(socket_ctx *ctx, const void *q, const void *K, const voi
     if (out_dtype != SOCKET_F32 && out_dtype != SOCKET_BF16) return SOCKET_EINVAL;
     return launch_dense_decode(ctx, q, K, V, block_table, seq_len, batch, scale, out_dtype, out,
                                (hipStream_t)stream);
+}
+
+static bool finite_f(float x) { return x == x && x <= 3.4e38f && x >= -3.4e38f; }
+
+static bool mods_ok(const socket_attn_mods *m) {
+    return !m || (finite_f(m->softcap) && m->softcap >= 0.0f && m->window >= 0);
+}
+
+// rows of q, K, V and what is written beside them are read and written 16 bytes at a time
+static bool aligned16(std::initializer_list<const void *> ptrs) {
+    for (const void *p : ptrs)
+        if ((uintptr_t)p % 16) return false;
+    return true;
+}
+
+int socket_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void *V, const int32_t *block_table,
+                       const int32_t *row_begin, const int32_t *row_count, int32_t batch, int32_t max_rows,
+                       float scale, const socket_attn_mods *mods, int32_t out_dtype, void *out, float *lse,
+                       void *stream) {
+    if (!ctx || !q || !K || !V || !row_begin || !row_count || !out) return SOCKET_EINVAL;
+    if (!batch_ok(ctx, batch) || !paging_ok(ctx, block_table)) return SOCKET_EINVAL;
+    if (max_rows < 0 || max_rows > ctx->g.max_n || !finite_f(scale) || !mods_ok(mods)) return SOCKET_EINVAL;
+    if (out_dtype != SOCKET_BF16 && out_dtype != SOCKET_F32) return SOCKET_EINVAL;
+    if (!aligned16({q, K, V, out})) return SOCKET_EINVAL;
+    if (max_rows == 0) return SOCKET_OK;
+    return launch_attend_rows(ctx, q, K, V, block_table, row_begin, row_count, batch, max_rows, scale, mods,
+                              out_dtype, out, lse, (hipStream_t)stream);
+}
+
+int socket_key_mass(socket_ctx *ctx, const void *q, const void *K, const float *lse, const int32_t *block_table,
+                    const int32_t *row_begin, const int32_t *row_count, int32_t batch, int32_t max_rows,
+                    float scale, const socket_attn_mods *mods, float decay, int32_t last_rows, float *mass,
+                    void *stream) {
+    if (!ctx || !q || !K || !lse || !row_begin || !row_count || !mass) return SOCKET_EINVAL;
+    if (!batch_ok(ctx, batch) || !paging_ok(ctx, block_table)) return SOCKET_EINVAL;
+    if (max_rows < 0 || max_rows > ctx->g.max_n || !finite_f(scale) || !mods_ok(mods)) return SOCKET_EINVAL;
+    if (!finite_f(decay) || decay < 0.0f || last_rows < 0 || !aligned16({q, K})) return SOCKET_EINVAL;
+    if (max_rows == 0) return SOCKET_OK;
+    return launch_key_mass(ctx, q, K, lse, block_table, row_begin, row_count, batch, max_rows, scale, mods, decay,
+                           last_rows, mass, (hipStream_t)stream);
+}
+
+int socket_evict_select(socket_ctx *ctx, const float *mass, const int32_t *block_table, const int32_t *seq_len,
+                        const int32_t *keep, int32_t batch, int32_t pool, float *scores, int32_t *idx,
+                        int32_t *n_selected, void *stream) {
+    if (!ctx || !mass || !seq_len || !keep || !scores || !idx || !n_selected) return SOCKET_EINVAL;
+    if (!batch_ok(ctx, batch) || !paging_ok(ctx, block_table)) return SOCKET_EINVAL;
+    if (pool < 1 || pool > 255 || pool % 2 == 0 || mass == scores) return SOCKET_EINVAL;
+    int rc = drop_pending(ctx, (hipStream_t)stream);
+    if (rc != SOCKET_OK) return rc;
+    rc = launch_evict_scores(ctx, mass, block_table, seq_len, batch, pool, scores, (hipStream_t)stream);
+    if (rc != SOCKET_OK) return rc;
+    return launch_topk(ctx, scores, seq_len, keep, batch, idx, n_selected, sk::kHistNone, (hipStream_t)stream);
+}
+
+int socket_evict_rows(socket_ctx *ctx, const int32_t *idx, const int32_t *n_selected, int32_t batch,
+                      const void *K, const void *V, const void *codes, const float *vnorm, const float *mass,
+                      const int32_t *block_table, void *K_out, void *V_out, void *codes_out, float *vnorm_out,
+                      float *mass_out, const int32_t *block_table_out, void *stream) {
+    if (!ctx || !idx || !n_selected || !K || !V || !K_out || !V_out) return SOCKET_EINVAL;
+    if (!codes != !codes_out || !vnorm != !vnorm_out || !mass != !mass_out) return SOCKET_EINVAL;
+    if (!batch_ok(ctx, batch) || !paging_ok(ctx, block_table) || !paging_ok(ctx, block_table_out)) return SOCKET_EINVAL;
+    if (!aligned16({K, V, K_out, V_out, codes, codes_out})) return SOCKET_EINVAL;
+    return launch_evict_rows(ctx, idx, n_selected, batch, K, V, codes, vnorm, mass, block_table, K_out, V_out,
+                             codes_out, vnorm_out, mass_out, block_table_out, (hipStream_t)stream);
 }
 
 int socket_decode_step(socket_ctx *ctx, const void *q, const void *K, const void *V, void *codes,

@@ -98,7 +98,8 @@ struct socket_ctx {
     int32_t *staged;      // [max_batch*Hkv][max_k] candidates picked by the long-list refinement
     int32_t *sel_regions; // [max_batch*Hkv][n_regions][kSlice] positions selected outright, by region of the sweep
     uint32_t *sel_cnt;    // [max_batch*Hkv][n_regions] how many each region holds
-    float *partials;      // [max_batch*Hq][n_split][d+2]
+    float *partials;      // [max_batch*Hq][n_split][d+2]; runs of rows: [batch][max_rows][Hq][n_split][d+2]
+    int64_t partial_floats;   // floats in partials
     int32_t *seq_scratch; // [max_batch] lengths after the append of a fused decode step
 };
 
@@ -161,6 +162,21 @@ int launch_sparse_decode(socket_ctx *ctx, const void *q, const void *K, const vo
 int sparse_decode_noalloc(const socket_params *p, const void *q, const void *K, const void *V,
                           const int32_t *idx, const int32_t *n_selected, const int32_t *block_table,
                           int batch, float scale, int out_dtype, void *out, hipStream_t st, int *hip_error);
+
+int attend_prepare(int d, int kv_dtype);   // once per context: LDS limits of the kernels for runs of rows
+int mass_prepare(int d, int kv_dtype);
+int launch_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void *V, const int32_t *block_table,
+                       const int32_t *row_begin, const int32_t *row_count, int batch, int max_rows, float scale,
+                       const socket_attn_mods *mods, int out_dtype, void *out, float *lse, hipStream_t st);
+int launch_key_mass(socket_ctx *ctx, const void *q, const void *K, const float *lse, const int32_t *block_table,
+                    const int32_t *row_begin, const int32_t *row_count, int batch, int max_rows, float scale,
+                    const socket_attn_mods *mods, float decay, int last_rows, float *mass, hipStream_t st);
+int launch_evict_scores(socket_ctx *ctx, const float *mass, const int32_t *block_table, const int32_t *seq_len, int batch,
+                        int pool, float *scores, hipStream_t st);
+int launch_evict_rows(socket_ctx *ctx, const int32_t *idx, const int32_t *n_selected, int batch,
+                      const void *K, const void *V, const void *codes, const float *vnorm, const float *mass,
+                      const int32_t *block_table, void *K_out, void *V_out, void *codes_out, float *vnorm_out,
+                      float *mass_out, const int32_t *block_table_out, hipStream_t st);
 
 // ---- device helpers -------------------------------------------------------------------
 
