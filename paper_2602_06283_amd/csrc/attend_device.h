@@ -144,6 +144,27 @@ template <typename T> __device__ __forceinline__ u32x4_t turn_sign(u32x4_t v, ui
     return v ^ s;
 }
 
+// the same for tiles of 16 rows (lane = column lane % 16; sixteenth of the wavefront g = lane / 16): a
+// k-step of bf16 takes piece 4 c + g, four k-steps of fp32 do
+typedef float floatx4v_t __attribute__((ext_vector_type(4)));
+template <typename T> __device__ __forceinline__ void mma_piece16(floatx4v_t &c, u32x4_t a, u32x4_t b);
+template <> __device__ __forceinline__ void mma_piece16<uint16_t>(floatx4v_t &c, u32x4_t a, u32x4_t b) {
+    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v_t, a), __builtin_bit_cast(bf16x8v_t, b), c, 0, 0, 0);
+}
+template <> __device__ __forceinline__ void mma_piece16<float>(floatx4v_t &c, u32x4_t a, u32x4_t b) {
+    const f32x4_t x = __builtin_bit_cast(f32x4_t, a), y = __builtin_bit_cast(f32x4_t, b);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
+}
+
+// max over the four sixteenths of a wavefront
+__device__ __forceinline__ float sixteenths_max(float v) {
+    auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 // sizes and swizzles of the K / V tiles in LDS, in pieces of 16 bytes
 template <typename T, int D> struct KvTile {
     static constexpr int KT = sizeof(T) == 2 ? 64 : 32;          // keys

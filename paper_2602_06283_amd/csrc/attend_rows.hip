@@ -38,7 +38,7 @@ struct RowsArgs {
     const int32_t *row_count;
     RowMap map;
     RowMods mods;
-    int BH, Hq, G, g_log2, max_rows, n_tiles, n_split, out_dtype;
+    int batch, BH, Hq, G, g_log2, max_rows, n_tiles, n_split, out_dtype;
 };
 
 // where a query's result goes: its index among all (sequence, row, query head)
@@ -408,6 +408,296 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_ke
     }
 }
 
+// ---- few rows: at most 16 NQ queries (rows times query heads) to a KV head, so K and V are read for
+// nothing else and what counts is bytes in flight.  A workgroup is one wavefront with a share of the keys
+// of its own: 32 rows of K and V (16 of wide fp32 rows) come into registers, coalesced, while it works
+// on the 32 before them, which lie in its LDS; no barriers.  16 x 16 tiles: keys by queries, then
+// channels by queries.
+template <typename T, int D> struct FewTile {
+    static constexpr int ROWB = D * (int)sizeof(T), CPR = ROWB / 16;
+    static constexpr int KT = sizeof(T) == 2 || D == 64 ? 32 : 16, NT = KT / 16;
+    static constexpr int BYTES = KT * ROWB, LOADS = KT * CPR / 64;
+    static __device__ __forceinline__ int k_piece(int row, int c) { return row * CPR + (c ^ (row & (CPR < 16 ? CPR - 1 : 15))); }
+    // bf16: four rows of 32 bytes are read at once; fp32: rows 4 g + r of four g, 64 bytes each
+    static __device__ __forceinline__ int v_piece(int row, int c) {
+        return row * CPR + (c ^ (sizeof(T) == 2 ? (row & 3) << 1 : ((row >> 2) & 3) << 2));
+    }
+};
+
+template <typename T, int D, int NQ, int PX>
+__global__ __launch_bounds__(64) void attend_few_kernel(RowsArgs a) {
+    using Tile = FewTile<T, D>;
+    constexpr int KT = Tile::KT, NT = Tile::NT, CPR = Tile::CPR, LOADS = Tile::LOADS, NKS = CPR / 4, NCB = D / 16;
+    constexpr int RPL = 64 / CPR > 0 ? 64 / CPR : 1;             // rows per load (wide rows: a part of one)
+    extern __shared__ __align__(16) char few_tiles[];            // K, V
+    char *const kt = few_tiles, *const vt = few_tiles + Tile::BYTES;
+
+    const int lane = threadIdx.x, g = lane >> 4;
+    const int bh = (int)blockIdx.x % a.BH, split = (int)blockIdx.x / a.BH;
+    const int b = bh / a.map.Hkv, h = bh - b * a.map.Hkv;
+    const RowRun run(a.row_begin, a.row_count, b, a.max_rows, a.map.max_n);
+    const int n_m = run.count * a.G;
+    if (n_m == 0) return;
+
+    // ---- queries of column block x: m = 16 x + lane % 16
+    int lo[NQ], hi[NQ], lo_w = 0x7fffffff, hi_w = -1;
+    u32x4_t q[NQ][NKS];
+    float slope2[NQ];
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+        const int m = 16 * x + (lane & 15);
+        lo[x] = 0x7fffffff;
+        hi[x] = -1;
+        slope2[x] = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) q[x][ks] = 0;
+        if (m < n_m) {
+            row_span(a.mods, b, run.begin + (m >> a.g_log2), run.len(), a.map.max_n, lo[x], hi[x]);
+            const char *src = (const char *)a.q + query_at(a, b, h, m) * Tile::ROWB;
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks) q[x][ks] = turn_sign<T>(*(const u32x4_t *)(src + (4 * ks + g) * 16), a.mods.sign);
+            if (a.mods.slopes) slope2[x] = a.mods.slopes[h * a.G + (m & (a.G - 1))] * kLog2e;
+            if (lo[x] <= hi[x]) {
+                lo_w = min(lo_w, lo[x]);
+                hi_w = max(hi_w, hi[x]);
+            }
+        }
+    }
+    // the longest span of the batch decides how many keys a split takes: the same for all sequences, so that
+    // those of a long one are not behind at the end
+    int longest = 0;
+    for (int y = lane; y < a.batch; y += 64) {
+        const int begin = a.row_begin[y], count = min(a.row_count[y], a.max_rows);
+        if (begin >= 0 && begin < a.map.max_n && count > 0) {
+            int span = min(begin + count, a.map.max_n);
+            if (a.mods.window > 0 && a.mods.window < span) span = min(span, a.mods.window + count - 1);
+            longest = max(longest, span);
+        }
+    }
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+        lo_w = min(lo_w, __shfl_xor(lo_w, o));
+        hi_w = max(hi_w, __shfl_xor(hi_w, o));
+        longest = max(longest, __shfl_xor(longest, o));
+    }
+    const int k_hi = __builtin_amdgcn_readfirstlane(hi_w);
+    const int base = __builtin_amdgcn_readfirstlane(lo_w & ~15);
+    const int n_tiles = k_hi >= 0 ? (k_hi - base) / KT + 1 : 0;
+    const int share = ((longest + 15 + KT - 1) / KT + a.n_split - 1) / a.n_split;
+    const int per = __builtin_amdgcn_readfirstlane(max(share, 64 / KT));
+    const int t_begin = min(n_tiles, split * per), t_end = min(n_tiles, t_begin + per);
+
+    // ---- rows of a tile, sixteen by sixteen (a block holds whole sixteens)
+    u32x4_t kreg[LOADS], vreg[LOADS];
+    int blk[NT], gone = 0, gone_next = 0;            // blocks of the tile that is loaded next; sixteenths without one
+    auto look_up = [&](int tile) __attribute__((always_inline)) {
+#pragma unroll
+        for (int y = 0; y < NT; ++y) {
+            blk[y] = 0;
+            if (a.map.block_table && tile < t_end)
+                blk[y] = scalar_load(&a.map.block_table[(int64_t)b * a.map.max_blocks + a.map.page_slot(min(base + tile * KT + 16 * y, k_hi))]);
+        }
+    };
+    auto load = [&](int tile) __attribute__((always_inline)) {
+        gone_next = 0;
+#pragma unroll
+        for (int y = 0; y < NT; ++y) {
+            const int first = min(base + tile * KT + 16 * y, k_hi & ~15);     // of the sixteen
+            int64_t at;
+            if (a.map.block_table) {
+                const bool absent = (unsigned)blk[y] >= (unsigned)a.map.num_blocks;
+                gone_next |= absent << y;
+                at = ((int64_t)(absent ? 0 : blk[y]) * a.map.Hkv + h) * a.map.page + a.map.page_off(first);
+            } else {
+                at = (int64_t)bh * a.map.max_n + first;
+            }
+            const char *ks = (const char *)a.K + at * Tile::ROWB, *vs = (const char *)a.V + at * Tile::ROWB;
+            const int last = k_hi - first;           // rows behind the last key read it again
+#pragma unroll
+            for (int p = 0; p < LOADS / NT; ++p) {
+                const int id = p * 64 + lane;
+                const uint32_t off = (uint32_t)(min(id / CPR, last) * Tile::ROWB + id % CPR * 16);
+                kreg[y * (LOADS / NT) + p] = *(const u32x4_t *)(ks + off);
+                vreg[y * (LOADS / NT) + p] = *(const u32x4_t *)(vs + off);
+            }
+        }
+    };
+    static_assert(16 % RPL == 0, "a load stays within a sixteen");
+
+    floatx4v_t o[NQ][NCB];
+    float top[NQ], sum[NQ];
+    const float ninf = -__builtin_inff();
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+        top[x] = ninf;
+        sum[x] = 0.0f;
+#pragma unroll
+        for (int cb = 0; cb < NCB; ++cb) o[x][cb] = 0.0f;
+    }
+    if (t_begin < t_end) {
+        look_up(t_begin);
+        load(t_begin);
+        look_up(t_begin + 1);
+    }
+    for (int tile = t_begin; tile < t_end; ++tile) {
+#pragma unroll
+        for (int p = 0; p < LOADS; ++p) {
+            const int id = p * 64 + lane, row = id / CPR, c = id % CPR;
+            *(u32x4_t *)(kt + Tile::k_piece(row, c) * 16) = kreg[p];
+            *(u32x4_t *)(vt + Tile::v_piece(row, c) * 16) = vreg[p];
+        }
+        gone = gone_next;
+        if (tile + 1 < t_end) {
+            load(tile + 1);
+            look_up(tile + 2);
+        }
+        const int t0 = base + tile * KT;
+        // ---- logits
+        float s[NQ][4 * NT];
+        {
+            floatx4v_t c[NQ][NT];
+#pragma unroll
+            for (int x = 0; x < NQ; ++x)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) c[x][t] = 0.0f;
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const u32x4_t kf = *(const u32x4_t *)(kt + Tile::k_piece(16 * t + (lane & 15), 4 * ks + g) * 16);
+#pragma unroll
+                    for (int x = 0; x < NQ; ++x) mma_piece16<T>(c[x][t], kf, q[x][ks]);
+                }
+#pragma unroll
+            for (int x = 0; x < NQ; ++x)
+#pragma unroll
+                for (int e = 0; e < 4 * NT; ++e) s[x][e] = c[x][e / 4][e % 4];
+        }
+#pragma unroll
+        for (int x = 0; x < NQ; ++x) {
+            float cc = a.mods.c;
+            if (a.mods.general) {
+                const int i = run.begin + ((16 * x + (lane & 15)) >> a.g_log2);
+                logits2(a.mods, s[x], (float)(i - t0), slope2[x], [&](int e) { return 16 * (e / 4) + 4 * g + e % 4; });
+                cc = 1.0f;
+            }
+            if (__any(lo[x] > t0 || hi[x] < t0 + KT - 1) || gone) {
+                const uint32_t span = (uint32_t)(hi[x] - lo[x]);
+                const bool any = lo[x] <= hi[x];
+#pragma unroll
+                for (int e = 0; e < 4 * NT; ++e) {
+                    const bool vis = any && (uint32_t)(t0 + 16 * (e / 4) + 4 * g + e % 4 - lo[x]) <= span && !((gone >> (e / 4)) & 1);
+                    s[x][e] = vis ? s[x][e] : ninf;
+                }
+            }
+            float mx = s[x][0];
+#pragma unroll
+            for (int e = 1; e < 4 * NT; ++e) mx = fmaxf(mx, s[x][e]);
+            mx = sixteenths_max(mx);
+            const float top_new = fmaxf(top[x], mx == ninf ? ninf : mx * cc);
+            const float use = top_new == ninf ? 0.0f : top_new;
+            if (__any(top_new > top[x])) {
+                const float alpha = exp2_fast(top[x] - use);
+                sum[x] *= alpha;
+#pragma unroll
+                for (int cb = 0; cb < NCB; ++cb) o[x][cb] *= alpha;
+            }
+            top[x] = top_new;
+            float part = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4 * NT; ++e) {
+                s[x][e] = exp2_fast(fmaf(s[x][e], cc, -use));
+                part += s[x][e];
+            }
+            sum[x] += part;
+        }
+        // ---- values
+        if constexpr (sizeof(T) == 2) {
+            u32x4_t w[NQ][PX];
+#pragma unroll
+            for (int x = 0; x < NQ; ++x)
+#pragma unroll
+                for (int y = 0; y < PX; ++y)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        w[x][y][e] = pack_bf16(s[x][2 * e], s[x][2 * e + 1]);
+                        if (y + 1 < PX) {
+                            s[x][2 * e] -= __uint_as_float(w[x][y][e] << 16);
+                            s[x][2 * e + 1] -= __uint_as_float(w[x][y][e] & 0xffff0000u);
+                        }
+                    }
+            const int row = 4 * g + ((lane & 15) >> 2), c0 = (lane & 3) >> 1, in = (lane & 1) * 8;
+#pragma unroll
+            for (int cb = 0; cb < NCB; ++cb) {
+                union { shortx4_t h[2]; u32x4_t v; } f;
+                f.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vt + Tile::v_piece(row, c0 + 2 * cb) * 16 + in));
+                f.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(vt + Tile::v_piece(row + 16, c0 + 2 * cb) * 16 + in));
+#pragma unroll
+                for (int x = 0; x < NQ; ++x)
+#pragma unroll
+                    for (int y = 0; y < PX; ++y) mma_piece16<uint16_t>(o[x][cb], f.v, w[x][y]);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4 * NT; ++e) {
+                const int row = 16 * (e / 4) + 4 * g + e % 4, ch = lane & 15;
+#pragma unroll
+                for (int cb = 0; cb < NCB; ++cb) {
+                    const float v = *(const float *)(vt + Tile::v_piece(row, 4 * cb + (ch >> 2)) * 16 + (ch & 3) * 4);
+#pragma unroll
+                    for (int x = 0; x < NQ; ++x) o[x][cb] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, s[x][e], o[x][cb], 0, 0, 0);
+                }
+            }
+        }
+    }
+
+    // ---- results
+#pragma unroll
+    for (int x = 0; x < NQ; ++x) {
+        const int m = 16 * x + (lane & 15);
+        const float total = xor32_sum(xor16_sum(sum[x]));
+        float check = 0.0f * total;
+#pragma unroll
+        for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) check = fmaf(0.0f, o[x][cb][r], check);
+        unsigned long long again = __ballot(m < n_m && !(check == 0.0f));
+        again |= again >> 32;
+        again = (again | (again >> 16)) & 0xffffull;
+        if (m < n_m && !((again >> (lane & 15)) & 1ull)) {
+            const int64_t at = query_at(a, b, h, m);
+            if (a.n_split > 1) {
+                float *part = a.partials + (at * a.n_split + split) * (D + 2);
+                if (g == 0) *(float2 *)part = make_float2(top[x], total);
+                if (t_begin < t_end) {
+#pragma unroll
+                    for (int cb = 0; cb < NCB; ++cb) {
+                        *(float2 *)(part + 2 + 16 * cb + 4 * g) = make_float2(o[x][cb][0], o[x][cb][1]);
+                        *(float2 *)(part + 4 + 16 * cb + 4 * g) = make_float2(o[x][cb][2], o[x][cb][3]);
+                    }
+                }
+            } else {
+                const float inv = total == 0.0f ? 0.0f : 1.0f / total;
+#pragma unroll
+                for (int cb = 0; cb < NCB; ++cb) {
+                    const f32x4_t y = {o[x][cb][0] * inv, o[x][cb][1] * inv, o[x][cb][2] * inv, o[x][cb][3] * inv};
+                    if (a.out_dtype == SOCKET_F32) *(f32x4_t *)((float *)a.out + at * D + 16 * cb + 4 * g) = y;
+                    else *(uint2 *)((uint16_t *)a.out + at * D + 16 * cb + 4 * g) = make_uint2(pack_bf16(y.x, y.y), pack_bf16(y.z, y.w));
+                }
+                if (a.lse && g == 0) a.lse[at] = total == 0.0f ? ninf : (top[x] + __builtin_amdgcn_logf(total)) * kLn2;
+            }
+        }
+        while (again) {
+            const int n = __builtin_ctzll(again);
+            again &= again - 1;
+            const int mq = 16 * x + n;
+            const int nlo = max(__builtin_amdgcn_readlane(lo[x], n), base + t_begin * KT);
+            const int nhi = min(__builtin_amdgcn_readlane(hi[x], n), base + t_end * KT - 1);
+            attend_plain<T, D>(a, b, h, mq, run.begin + (mq >> a.g_log2), nlo, nhi, split);
+        }
+    }
+}
+
 // Joins the splits of one query: out = sum_s w_s acc_s / sum_s w_s l_s, w_s = exp2(m_s - max m).
 constexpr int kRowsMergeThreads = 256;
 template <int D>
@@ -487,6 +777,27 @@ template <typename T, int D> static void launch_rows(const RowsArgs &a, dim3 gri
     hipLaunchKernelGGL((attend_rows_kernel<T, D, 1>), grid, dim3(kRowsThreads), lds, st, a);
 }
 
+template <typename T, int D> static void launch_few(const RowsArgs &a, bool wide, dim3 grid, hipStream_t st) {
+    constexpr size_t lds = 2 * FewTile<T, D>::BYTES;
+    static_assert(lds <= 64 * 1024, "within the default dynamic LDS limit");
+    if constexpr (sizeof(T) == 2) {
+        if (a.out_dtype == SOCKET_F32) {
+            if (wide) hipLaunchKernelGGL((attend_few_kernel<T, D, 2, 3>), grid, dim3(64), lds, st, a);
+            else hipLaunchKernelGGL((attend_few_kernel<T, D, 1, 3>), grid, dim3(64), lds, st, a);
+            return;
+        }
+    }
+    if (wide) hipLaunchKernelGGL((attend_few_kernel<T, D, 2, 1>), grid, dim3(64), lds, st, a);
+    else hipLaunchKernelGGL((attend_few_kernel<T, D, 1, 1>), grid, dim3(64), lds, st, a);
+}
+
+static int pick_splits(int64_t wanted, int64_t most, int64_t room) {
+    int64_t n = wanted < most ? wanted : most;
+    n = n < room ? n : room;
+    n = n < kMaxSplits ? n : kMaxSplits;
+    return n < 1 ? 1 : (int)n;
+}
+
 int launch_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void *V, const int32_t *block_table,
                        const int32_t *row_begin, const int32_t *row_count, int batch, int max_rows, float scale,
                        const socket_attn_mods *mods, int out_dtype, void *out, float *lse, hipStream_t st) {
@@ -498,26 +809,39 @@ int launch_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void
     a.mods = row_mods(scale, mods);
     a.BH = batch * g.Hkv; a.Hq = g.Hq; a.G = g.G; a.g_log2 = __builtin_ctz((unsigned)g.G);
     a.max_rows = max_rows; a.out_dtype = out_dtype;
-    a.n_tiles = (int)(((int64_t)max_rows * g.G + kRowsQueries - 1) / kRowsQueries);
-    // Two workgroups per compute unit keep it busy; with fewer the keys are split, down to four tiles each
-    // and as far as the partial results fit.
-    const int64_t wgs = (int64_t)a.BH * a.n_tiles;
-    const int64_t room = ctx->partial_floats / ((int64_t)batch * max_rows * g.Hq * (g.d + 2));
-    int64_t n = 512 / wgs;
-    const int64_t most = (g.max_n + 255) / 256;
-    n = n < most ? n : most;
-    n = n < room ? n : room;
-    n = n < kMaxSplits ? n : kMaxSplits;
-    a.n_split = n < 1 ? 1 : (int)n;
-    const int64_t grid = wgs * a.n_split;
-    if (grid >= (int64_t)1 << 31) return SOCKET_EUNSUPPORTED;
+    a.batch = batch;
+    const int64_t room = ctx->partial_floats / ((int64_t)batch * max_rows * g.Hq * (g.d + 2));   // splits whose results fit
     const bool f32 = g.kv_dtype == SOCKET_F32;
-    const dim3 gr((unsigned)grid);
-    switch (g.d) {
-        case 64: f32 ? launch_rows<float, 64>(a, gr, st) : launch_rows<uint16_t, 64>(a, gr, st); break;
-        case 128: f32 ? launch_rows<float, 128>(a, gr, st) : launch_rows<uint16_t, 128>(a, gr, st); break;
-        case 256: f32 ? launch_rows<float, 256>(a, gr, st) : launch_rows<uint16_t, 256>(a, gr, st); break;
-        default: return SOCKET_EUNSUPPORTED;
+    if ((int64_t)max_rows * g.G <= 32) {
+        // One wavefront a split, at least 64 keys each: with 16 and more of them to a compute unit the last
+        // ones to finish are a small part.
+        a.n_tiles = 1;
+        a.n_split = pick_splits(8192 / a.BH, (g.max_n + 63) / 64, room);
+        const int64_t grid = (int64_t)a.BH * a.n_split;
+        if (grid >= (int64_t)1 << 31) return SOCKET_EUNSUPPORTED;
+        const dim3 gr((unsigned)grid);
+        const bool wide = max_rows * g.G > 16;
+        switch (g.d) {
+            case 64: f32 ? launch_few<float, 64>(a, wide, gr, st) : launch_few<uint16_t, 64>(a, wide, gr, st); break;
+            case 128: f32 ? launch_few<float, 128>(a, wide, gr, st) : launch_few<uint16_t, 128>(a, wide, gr, st); break;
+            case 256: f32 ? launch_few<float, 256>(a, wide, gr, st) : launch_few<uint16_t, 256>(a, wide, gr, st); break;
+            default: return SOCKET_EUNSUPPORTED;
+        }
+    } else {
+        // Two workgroups per compute unit keep it busy; with fewer the keys are split, down to four tiles each
+        // and as far as the partial results fit.
+        a.n_tiles = (int)(((int64_t)max_rows * g.G + kRowsQueries - 1) / kRowsQueries);
+        const int64_t wgs = (int64_t)a.BH * a.n_tiles;
+        a.n_split = pick_splits(512 / wgs, (g.max_n + 255) / 256, room);
+        const int64_t grid = wgs * a.n_split;
+        if (grid >= (int64_t)1 << 31) return SOCKET_EUNSUPPORTED;
+        const dim3 gr((unsigned)grid);
+        switch (g.d) {
+            case 64: f32 ? launch_rows<float, 64>(a, gr, st) : launch_rows<uint16_t, 64>(a, gr, st); break;
+            case 128: f32 ? launch_rows<float, 128>(a, gr, st) : launch_rows<uint16_t, 128>(a, gr, st); break;
+            case 256: f32 ? launch_rows<float, 256>(a, gr, st) : launch_rows<uint16_t, 256>(a, gr, st); break;
+            default: return SOCKET_EUNSUPPORTED;
+        }
     }
     if (a.n_split > 1) {
         const dim3 mg(g.Hq, max_rows, batch);
