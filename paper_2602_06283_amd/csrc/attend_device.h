@@ -117,6 +117,24 @@ __device__ __forceinline__ void logits2(const RowMods &m, float (&x)[N], float i
     }
 }
 
+// Rows of one (sequence, KV head) by block, without a branch: a contiguous cache is a single block, 0.
+struct BlockRows {
+    int64_t stride, base;
+    int blocks, page;
+    uint32_t page_magic;
+    __device__ __forceinline__ BlockRows(const RowMap &m, int b, int h) {
+        const bool paged = m.block_table != nullptr;
+        stride = paged ? (int64_t)m.Hkv * m.page : 0;
+        base = paged ? (int64_t)h * m.page : ((int64_t)b * m.Hkv + h) * m.max_n;
+        blocks = paged ? m.num_blocks : 1;
+        page = paged ? m.page : 0;
+        page_magic = paged ? m.page_magic : 0u;
+    }
+    __device__ __forceinline__ int64_t at(int blk, int t) const {
+        return blk * stride + base + (t - (int)__umulhi((uint32_t)t, page_magic) * page);
+    }
+};
+
 // ---- matrix tiles: 32 keys x 32 queries, logits as K Q^T, so that a lane holds one query's
 // logits and the softmax runs along its registers
 typedef float floatx16_t __attribute__((ext_vector_type(16)));
@@ -172,14 +190,15 @@ template <typename T, int D> struct KvTile {
     static constexpr int CPR = ROWB / 16;                        // pieces per row
     static constexpr int BYTES = KT * ROWB;
     // K: 32 rows are read at one piece each: the piece is turned by the row
-    static __device__ __forceinline__ int k_piece(int row, int c) { return row * CPR + (c ^ (row & (CPR < 16 ? CPR - 1 : 15))); }
+    static __device__ __forceinline__ int k_turned(int row, int c) { return c ^ (row & (CPR < 16 ? CPR - 1 : 15)); }
+    static __device__ __forceinline__ int k_piece(int row, int c) { return row * CPR + k_turned(row, c); }
     // V: bf16 rows are read four at a time, 64 bytes each, and transposed on the way; fp32 rows r and
     // r + 4 at once, 128 bytes each
-    static __device__ __forceinline__ int v_turn(int row) {
-        if (sizeof(T) == 4) return ((row >> 2) & 1) << 3;
-        return CPR == 8 ? ((row >> 1) & 1) << 2 : (row & 3) << 2;
+    static __device__ __forceinline__ int v_turned(int row, int c) {
+        if (sizeof(T) == 4) return c ^ (((row >> 2) & 1) << 3);
+        return c ^ (CPR == 8 ? ((row >> 1) & 1) << 2 : (row & 3) << 2);
     }
-    static __device__ __forceinline__ int v_piece(int row, int c) { return row * CPR + (c ^ v_turn(row)); }
+    static __device__ __forceinline__ int v_piece(int row, int c) { return row * CPR + v_turned(row, c); }
 };
 
 }  // namespace sk

@@ -180,7 +180,12 @@ template <int D, int PX> struct ValueProduct<float, D, PX> {
     }
 };
 
-template <typename T, int D> constexpr size_t rows_lds() { return (size_t)4 * KvTile<T, D>::BYTES; }
+// 16 bytes a lane from memory to LDS, at `to` + 16 lane (`to` is the same for the wavefront)
+__device__ __forceinline__ void lds_fill(const char *from, char *to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+
+constexpr float kTopSlack = 8.0f;
 
 template <typename T, int D, int PX>
 __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_kernel(RowsArgs a) {
@@ -188,9 +193,9 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_ke
     constexpr int KT = Tile::KT, CPR = Tile::CPR, NU = KT / 32, NG = KT / 16;
     constexpr int LOADS = KT * CPR / kRowsThreads;               // pieces of K (and of V) a thread brings
     constexpr int NKS = CPR / 2;                                 // pairs of pieces along the channels
-    extern __shared__ __align__(16) char rows_tiles[];           // [2][K tile, V tile]
+    __shared__ __align__(16) char s_k0[Tile::BYTES], s_v0[Tile::BYTES], s_k1[Tile::BYTES], s_v1[Tile::BYTES];
+    __shared__ __align__(16) int s_absent0[4], s_absent1[4];     // sixteenths of a tile whose block is absent
     __shared__ int s_lo[4], s_hi[4];
-    __shared__ __align__(16) int s_absent[2][4];                 // sixteenths of a tile whose block is absent
 
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hf = lane >> 5;
     // all workgroups of a KV head on one XCD where there are eight heads or more (its L2 then serves the
@@ -238,38 +243,37 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_ke
     const int per = (n_tiles + a.n_split - 1) / a.n_split;
     const int t_begin = split * per, t_end = min(n_tiles, t_begin + per);
 
-    // ---- staging: 16-byte pieces of 64 / CPR rows per wavefront and load, all of them in one sixteenth
-    //      of the cache (a block holds whole ones), so the block is one scalar look-up
-    u32x4_t kreg[LOADS], vreg[LOADS];
-    bool absent[LOADS];
-    auto load = [&](int tile) __attribute__((always_inline)) {
+    // ---- staging, straight from memory into LDS: a load of a wavefront fills 64 pieces in a row there, so the
+    //      turn of the pieces is done in the address it reads.  Its rows lie in one sixteenth of the cache
+    //      (a block holds whole ones): one scalar look-up, made a tile ahead.  A buffer is an array of its own, and the
+    //      loop goes over both: the compiler then sees that reads of one need not wait for the other's loads.
+    const BlockRows rows(a.map, b, h);
+    int blk[LOADS];
+#pragma unroll
+    for (int p = 0; p < LOADS; ++p) blk[p] = 0;
+    auto look_up = [&](int tile) __attribute__((always_inline)) {
+        if (a.map.block_table == nullptr || tile >= t_end) return;
 #pragma unroll
         for (int p = 0; p < LOADS; ++p) {
-            const int id = p * kRowsThreads + tid, row = id / CPR, c = id % CPR;
-            const int t = min(base + tile * KT + row, k_hi);
-            int64_t at;
-            absent[p] = false;
-            if (a.map.block_table == nullptr) {
-                at = (int64_t)bh * a.map.max_n + t;
-            } else {
-                const int slot = a.map.page_slot(__builtin_amdgcn_readfirstlane(t));
-                int blk = scalar_load(&a.map.block_table[(int64_t)b * a.map.max_blocks + slot]);
-                absent[p] = (unsigned)blk >= (unsigned)a.map.num_blocks;
-                if (absent[p]) blk = 0;
-                at = ((int64_t)blk * a.map.Hkv + h) * a.map.page + (t - slot * a.map.page);
-            }
-            kreg[p] = *(const u32x4_t *)((const char *)a.K + at * Tile::ROWB + c * 16);
-            vreg[p] = *(const u32x4_t *)((const char *)a.V + at * Tile::ROWB + c * 16);
+            const int row = (p * kRowsThreads + wave * 64) / CPR;
+            const int t = __builtin_amdgcn_readfirstlane(min(base + tile * KT + row, k_hi));
+            blk[p] = scalar_load(&a.map.block_table[(int64_t)b * a.map.max_blocks + a.map.page_slot(t)]);
         }
     };
-    auto store = [&](int buf) __attribute__((always_inline)) {
-        char *kt = rows_tiles + buf * 2 * Tile::BYTES, *vt = kt + Tile::BYTES;
+    auto load = [&](int tile, char *kt, char *vt, int *absent) __attribute__((always_inline)) {
 #pragma unroll
         for (int p = 0; p < LOADS; ++p) {
-            const int id = p * kRowsThreads + tid, row = id / CPR, c = id % CPR;
-            *(u32x4_t *)(kt + Tile::k_piece(row, c) * 16) = kreg[p];
-            *(u32x4_t *)(vt + Tile::v_piece(row, c) * 16) = vreg[p];
-            if (c == 0 && (row & 15) == 0) s_absent[buf][row >> 4] = absent[p];
+            const int slot = p * kRowsThreads + wave * 64, row0 = slot / CPR;        // the wavefront's first piece and row
+            const int row = (slot + lane) / CPR, c = lane % CPR;
+            const int first = __builtin_amdgcn_readfirstlane(min((base + tile * KT + row0) & ~15, k_hi & ~15));
+            const bool gone = (unsigned)blk[p] >= (unsigned)rows.blocks;
+            const int64_t at = rows.at(gone ? 0 : blk[p], first);
+            if ((row0 & 15) == 0 && lane == 0) absent[row0 >> 4] = gone;
+            const int in = min(base + tile * KT + row, k_hi) - first;                // (rows behind the last key read it again)
+            const char *ks = (const char *)a.K + at * Tile::ROWB, *vs = (const char *)a.V + at * Tile::ROWB;
+            const uint32_t k_off = (uint32_t)(in * Tile::ROWB + Tile::k_turned(row, c) * 16), v_off = (uint32_t)(in * Tile::ROWB + Tile::v_turned(row, c) * 16);
+            lds_fill(ks + k_off, kt + slot * 16);
+            lds_fill(vs + v_off, vt + slot * 16);
         }
     };
 
@@ -278,29 +282,30 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_ke
     for (int cb = 0; cb < D / 32; ++cb) o[cb] = 0.0f;
     const float ninf = -__builtin_inff();
     float top = ninf, sum = 0.0f;                    // running maximum and this lane's half of the running sum
-    if (t_begin < t_end) {
-        load(t_begin);
-        store(0);
-    }
-    __syncthreads();
-    for (int tile = t_begin; tile < t_end; ++tile) {
-        const int buf = (tile - t_begin) & 1;
-        const char *kt = rows_tiles + buf * 2 * Tile::BYTES, *vt = kt + Tile::BYTES;
-        const bool more = tile + 1 < t_end;
-        if (more) load(tile + 1);
+
+    // one tile from (kt, vt), while the next one is on its way to (kn, vn)
+    auto tile_step = [&](int tile, const char *kt, const char *vt, const int *absent, char *kn, char *vn, int *absent_n) __attribute__((always_inline)) {
+        if (tile + 1 < t_end) {
+            load(tile + 1, kn, vn, absent_n);
+            look_up(tile + 2);
+        }
         const int t0 = base + tile * KT;
         if (__any(valid && lo <= t0 + KT - 1 && hi >= t0)) {
             // ---- logits
             float s[NU][16];
+            {
+                floatx16_t c[NU];
 #pragma unroll
-            for (int u = 0; u < NU; ++u) {
-                floatx16_t c = 0.0f;
-                const int row = 32 * u + (lane & 31);
+                for (int u = 0; u < NU; ++u) c[u] = 0.0f;
 #pragma unroll
                 for (int ks = 0; ks < NKS; ++ks)
-                    mma_piece<T>(c, *(const u32x4_t *)(kt + Tile::k_piece(row, 2 * ks + hf) * 16), q[ks]);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[u][r] = c[r];
+                    for (int u = 0; u < NU; ++u)
+                        mma_piece<T>(c[u], *(const u32x4_t *)(kt + Tile::k_piece(32 * u + (lane & 31), 2 * ks + hf) * 16), q[ks]);
+#pragma unroll
+                for (int u = 0; u < NU; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[u][r] = c[u][r];
             }
             float cc = a.mods.c;
             if (a.mods.general) {
@@ -313,7 +318,7 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_ke
             int gone = 0;
             if (a.map.block_table) {
 #pragma unroll
-                for (int g = 0; g < NG; ++g) gone |= s_absent[buf][g] << g;
+                for (int g = 0; g < NG; ++g) gone |= absent[g] << g;
                 gone = __builtin_amdgcn_readfirstlane(gone);
             }
             if (__any(valid && (lo > t0 || hi < t0 + KT - 1)) || gone) {
@@ -339,15 +344,18 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_ke
                 auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
                 mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
             }
-            const float top_new = fmaxf(top, mx == ninf ? ninf : mx * cc);
-            const float use = top_new == ninf ? 0.0f : top_new;
-            if (__any(top_new > top)) {
-                const float alpha = exp2_fast(top - use);
+            mx = mx == ninf ? ninf : mx * cc;
+            // (what the weights are taken against need not be the maximum itself: as long as none is above
+            // 2^8 it stays, and the sums with it)
+            if (__any(mx > top + kTopSlack)) {
+                const float top_new = fmaxf(top, mx);
+                const float alpha = top_new == ninf ? 1.0f : exp2_fast(top - top_new);
                 sum *= alpha;
 #pragma unroll
                 for (int cb = 0; cb < D / 32; ++cb) o[cb] *= alpha;
+                top = top_new;
             }
-            top = top_new;
+            const float use = top == ninf ? 0.0f : top;
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
                 float part = 0.0f;
@@ -362,8 +370,19 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_ke
 #pragma unroll
             for (int u = 0; u < NU; ++u) ValueProduct<T, D, PX>::run(o, vt, u, s[u], lane);
         }
-        if (more) store(buf ^ 1);
+        __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): this wavefront's part of the next tile is there
         __syncthreads();
+    };
+    if (t_begin < t_end) {
+        look_up(t_begin);
+        load(t_begin, s_k0, s_v0, s_absent0);
+        look_up(t_begin + 1);
+    }
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    __syncthreads();
+    for (int tile = t_begin; tile < t_end; tile += 2) {
+        tile_step(tile, s_k0, s_v0, s_absent0, s_k1, s_v1, s_absent1);
+        if (tile + 1 < t_end) tile_step(tile + 1, s_k1, s_v1, s_absent1, s_k0, s_v0, s_absent0);
     }
 
     // ---- results
@@ -488,6 +507,7 @@ __global__ __launch_bounds__(64) void attend_few_kernel(RowsArgs a) {
     const int t_begin = min(n_tiles, split * per), t_end = min(n_tiles, t_begin + per);
 
     // ---- rows of a tile, sixteen by sixteen (a block holds whole sixteens)
+    const BlockRows rows(a.map, b, h);
     u32x4_t kreg[LOADS], vreg[LOADS];
     int blk[NT], gone = 0, gone_next = 0;            // blocks of the tile that is loaded next; sixteenths without one
     auto look_up = [&](int tile) __attribute__((always_inline)) {
@@ -503,14 +523,9 @@ __global__ __launch_bounds__(64) void attend_few_kernel(RowsArgs a) {
 #pragma unroll
         for (int y = 0; y < NT; ++y) {
             const int first = min(base + tile * KT + 16 * y, k_hi & ~15);     // of the sixteen
-            int64_t at;
-            if (a.map.block_table) {
-                const bool absent = (unsigned)blk[y] >= (unsigned)a.map.num_blocks;
-                gone_next |= absent << y;
-                at = ((int64_t)(absent ? 0 : blk[y]) * a.map.Hkv + h) * a.map.page + a.map.page_off(first);
-            } else {
-                at = (int64_t)bh * a.map.max_n + first;
-            }
+            const bool absent = (unsigned)blk[y] >= (unsigned)rows.blocks;
+            gone_next |= absent << y;
+            const int64_t at = rows.at(absent ? 0 : blk[y], first);
             const char *ks = (const char *)a.K + at * Tile::ROWB, *vs = (const char *)a.V + at * Tile::ROWB;
             const int last = k_hi - first;           // rows behind the last key read it again
 #pragma unroll
@@ -748,33 +763,14 @@ __global__ __launch_bounds__(kRowsMergeThreads) void attend_rows_merge_kernel(Ro
     }
 }
 
-template <typename T, int D> static int rows_allow() {
-    constexpr size_t lds = rows_lds<T, D>();
-    if (lds <= 64 * 1024) return SOCKET_OK;
-    auto allow = [](auto kernel) {
-        return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess;
-    };
-    bool ok = allow(attend_rows_kernel<T, D, 1>);
-    if constexpr (sizeof(T) == 2) ok = ok && allow(attend_rows_kernel<T, D, 3>);
-    return ok ? SOCKET_OK : SOCKET_EHIP;
-}
-
-int attend_prepare(int d, int kv_dtype) {
-    const bool f32 = kv_dtype == SOCKET_F32;
-    return d == 64    ? (f32 ? rows_allow<float, 64>() : rows_allow<uint16_t, 64>())
-           : d == 128 ? (f32 ? rows_allow<float, 128>() : rows_allow<uint16_t, 128>())
-                      : (f32 ? rows_allow<float, 256>() : rows_allow<uint16_t, 256>());
-}
-
 template <typename T, int D> static void launch_rows(const RowsArgs &a, dim3 grid, hipStream_t st) {
-    constexpr size_t lds = rows_lds<T, D>();
     if constexpr (sizeof(T) == 2) {
         if (a.out_dtype == SOCKET_F32) {
-            hipLaunchKernelGGL((attend_rows_kernel<T, D, 3>), grid, dim3(kRowsThreads), lds, st, a);
+            hipLaunchKernelGGL((attend_rows_kernel<T, D, 3>), grid, dim3(kRowsThreads), 0, st, a);
             return;
         }
     }
-    hipLaunchKernelGGL((attend_rows_kernel<T, D, 1>), grid, dim3(kRowsThreads), lds, st, a);
+    hipLaunchKernelGGL((attend_rows_kernel<T, D, 1>), grid, dim3(kRowsThreads), 0, st, a);
 }
 
 template <typename T, int D> static void launch_few(const RowsArgs &a, bool wide, dim3 grid, hipStream_t st) {
