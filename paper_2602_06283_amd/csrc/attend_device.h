@@ -135,6 +135,11 @@ struct BlockRows {
     }
 };
 
+// 16 bytes a lane from memory to LDS, at `to` + 16 lane (`to` is the same for the wavefront)
+__device__ __forceinline__ void lds_fill(const char *from, char *to) {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+
 // ---- matrix tiles: 32 keys x 32 queries, logits as K Q^T, so that a lane holds one query's
 // logits and the softmax runs along its registers
 typedef float floatx16_t __attribute__((ext_vector_type(16)));

@@ -180,11 +180,6 @@ template <int D, int PX> struct ValueProduct<float, D, PX> {
     }
 };
 
-// 16 bytes a lane from memory to LDS, at `to` + 16 lane (`to` is the same for the wavefront)
-__device__ __forceinline__ void lds_fill(const char *from, char *to) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
-}
-
 constexpr float kTopSlack = 8.0f;
 
 template <typename T, int D, int PX>

@@ -213,7 +213,6 @@ int socket_create(socket_ctx **out, const socket_params *p) {
     ctx->partial_floats = sz_part / 4;
     ctx->scratch_bytes = sz_tables + sz_tstats + sz_sub + sz_hist + sz_cnt + 2 * sz_cand + sz_staged + sz_regions + sz_selcnt + sz_part + sz_seq;
     bool ok = score_prepare(g) == SOCKET_OK &&
-              mass_prepare(g.d, g.kv_dtype) == SOCKET_OK &&
               hipMalloc((void **)&ctx->tables, sz_tables) == hipSuccess &&
               hipMalloc((void **)&ctx->tstats, sz_tstats) == hipSuccess &&
               (sz_sub == 0 || hipMalloc((void **)&ctx->subprobs, sz_sub) == hipSuccess) &&

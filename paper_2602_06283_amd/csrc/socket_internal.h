@@ -163,7 +163,6 @@ int sparse_decode_noalloc(const socket_params *p, const void *q, const void *K, 
                           const int32_t *idx, const int32_t *n_selected, const int32_t *block_table,
                           int batch, float scale, int out_dtype, void *out, hipStream_t st, int *hip_error);
 
-int mass_prepare(int d, int kv_dtype);     // once per context: LDS limits
 int launch_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void *V, const int32_t *block_table,
                        const int32_t *row_begin, const int32_t *row_count, int batch, int max_rows, float scale,
                        const socket_attn_mods *mods, int out_dtype, void *out, float *lse, hipStream_t st);
