@@ -11,10 +11,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The caller's modifications of the scores, as the kernels take them.  Everything is in units of
 // log 2, so that a weight is one exp2.
 struct RowMods {
-    float c;              // |scale| log2(e) (the queries' signs are turned where scale < 0, which is exact)
-    uint32_t sign;        // 0x80000000 where they are
+    float c;              // scale log2(e)
     float y_scale, a;     // capped logits: a tanh(y_scale x), a = cap log2(e); a = 0: not capped
-    int general;          // capped, biased or scale = 0: logits are formed before the mask and the maximum
     int window;
     const float *slopes;
     const int32_t *prefix_len;
@@ -23,12 +21,10 @@ struct RowMods {
 
 inline RowMods row_mods(float scale, const socket_attn_mods *m) {
     RowMods r{};
-    const float s = scale < 0.0f ? -scale : scale;
-    r.sign = scale < 0.0f ? 0x80000000u : 0u;
-    r.c = s * kLog2e;
+    r.c = scale * kLog2e;
     if (m) {
         if (m->softcap > 0.0f) {
-            r.y_scale = s / m->softcap;
+            r.y_scale = scale / m->softcap;
             r.a = m->softcap * kLog2e;
         }
         r.window = m->window;
@@ -36,7 +32,6 @@ inline RowMods row_mods(float scale, const socket_attn_mods *m) {
         r.prefix_len = m->prefix_len;
         r.doc_begin = m->doc_begin;
     }
-    r.general = r.a > 0.0f || r.slopes != nullptr || r.c == 0.0f;
     return r;
 }
 
@@ -68,53 +63,69 @@ __device__ __forceinline__ void row_span(const RowMods &m, int b, int i, int len
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// tanh to about four units in the last place: its power series up to |y| = 1/4 (the first term left
-// out, 1382/155925 y^11, is 8e-9 of it there), beyond that 1 - 2 / (1 + e^2y), whose rounding is
-// absolute and would be felt only near zero.
-__device__ __forceinline__ float tanh_series(float y) {
-    const float z = y * y;
-    const float t = fmaf(fmaf(fmaf(fmaf(62.0f / 2835.0f, z, -17.0f / 315.0f), z, 2.0f / 15.0f), z, -1.0f / 3.0f), z, 1.0f);
-    return y * t;
+// tanh(y) / y up to |y| = 1/4, z = y^2: the power series 1 - z/3 + 2 z^2/15 - 17 z^3/315 + 62 z^4/2835, its
+// last term replaced by what is left of z^4 after a Chebyshev polynomial of degree four on [0, 1/16] is taken from it
+// (z^4 = z^3/8 - 5 z^2/1024 + z/16384 up to 1.2e-7, times 62/2835).  Off by 1.2e-8 at most, the series' own rest included.
+constexpr float kCapSmall = 0.25f;
+__device__ __forceinline__ float tanh_ratio(float z) {
+    constexpr double c4 = 62.0 / 2835.0;
+    constexpr float c3 = (float)(-17.0 / 315.0 + c4 / 8.0), c2 = (float)(2.0 / 15.0 - c4 * 5.0 / 1024.0), c1 = (float)(-1.0 / 3.0 + c4 / 16384.0);
+    return fmaf(fmaf(fmaf(c3, z, c2), z, c1), z, 1.0f);
 }
+// tanh for any y: beyond 1/4, 1 - 2 / (1 + e^2y), whose rounding is absolute and would be felt only near zero
 __device__ __forceinline__ float tanh_any(float y) {
     const float far = fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + exp2_fast(y * (2.0f * kLog2e))), 1.0f);
-    return fabsf(y) <= 0.25f ? tanh_series(y) : far;
+    return fabsf(y) <= kCapSmall ? y * tanh_ratio(y * y) : far;
 }
 
-// the logit (in units of log 2) of a dot product, at distance dist = i - j, slope2 = slope log2(e)
-__device__ __forceinline__ float logit2(const RowMods &m, float x, float dist, float slope2) {
-    float s = m.a > 0.0f ? m.a * tanh_any(x * m.y_scale) : x * m.c;
+// The logit of a dot product less `ref`, in units of log 2, at distance dist = i - j; slope2 = slope log2(e).
+__device__ __forceinline__ float logit2(const RowMods &m, float x, float dist, float slope2, float ref) {
+    float s = m.a > 0.0f ? fmaf(m.a, tanh_any(x * m.y_scale), -ref) : fmaf(x, m.c, -ref);
     if (m.slopes) s = fmaf(-slope2, fabsf(dist), s);
     return s;
 }
 
-// The same for the N dot products of one query that a lane holds of a tile, key of x[n] = key0 +
-// row_of(n): capped logits are mostly far below the cap, so a wavefront whose arguments all are
-// small takes the series alone.
-template <int N, typename F>
-__device__ __forceinline__ void logits2(const RowMods &m, float (&x)[N], float i_minus_key0, float slope2, F row_of) {
-    if (m.a > 0.0f) {
+// The same for the N dot products of one query that a lane holds of a tile, the key of x[n] being
+// key0 + row_of(n): capped logits are mostly far below the cap, so a wavefront whose arguments all are
+// small takes the ratio alone.  GEN: capped or biased.
+template <bool GEN, int N, typename F>
+__device__ __forceinline__ void logits2(const RowMods &m, float (&x)[N], float i_minus_key0, float slope2, float ref, F row_of) {
+    if (GEN && m.a > 0.0f) {
         float top = 0.0f;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
             x[n] *= m.y_scale;
             top = fmaxf(top, fabsf(x[n]));
         }
-        if (__all(top <= 0.25f)) {
+        if (__all(top <= kCapSmall)) {
 #pragma unroll
-            for (int n = 0; n < N; ++n) x[n] = m.a * tanh_series(x[n]);
+            for (int n = 0; n < N; ++n) x[n] = fmaf(x[n] * m.a, tanh_ratio(x[n] * x[n]), -ref);
         } else {
 #pragma unroll
-            for (int n = 0; n < N; ++n) x[n] = m.a * tanh_any(x[n]);
+            for (int n = 0; n < N; ++n) x[n] = fmaf(m.a, tanh_any(x[n]), -ref);
         }
     } else {
 #pragma unroll
-        for (int n = 0; n < N; ++n) x[n] *= m.c;
+        for (int n = 0; n < N; ++n) x[n] = fmaf(x[n], m.c, -ref);
     }
-    if (m.slopes) {
+    if (GEN && m.slopes) {
 #pragma unroll
         for (int n = 0; n < N; ++n) x[n] = fmaf(-slope2, fabsf(i_minus_key0 - (float)row_of(n)), x[n]);
     }
+}
+
+// Longest sequence of a batch, cut to what a window lets its rows see: by one wavefront.
+__device__ __forceinline__ int longest_of(const int32_t *row_begin, const int32_t *row_count, int batch, int max_rows, int max_n, int window) {
+    int longest = 0;
+    for (int y = (int)(threadIdx.x & 63); y < batch; y += 64) {
+        const int begin = row_begin[y], count = min(row_count[y], max_rows);
+        if (begin >= 0 && begin < max_n && count > 0) {
+            int span = min(begin + count, max_n);
+            if (window > 0 && window < span) span = min(span, window + count - 1);
+            longest = max(longest, span);
+        }
+    }
+    return (int)wave_max((float)longest);            // (exact: positions are below 2^24)
 }
 
 // Rows of one (sequence, KV head) by block, without a branch: a contiguous cache is a single block, 0.
@@ -159,12 +170,6 @@ template <> __device__ __forceinline__ void mma_piece<float>(floatx16_t &c, u32x
     const f32x4_t x = __builtin_bit_cast(f32x4_t, a), y = __builtin_bit_cast(f32x4_t, b);
 #pragma unroll
     for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], c, 0, 0, 0);
-}
-
-// turns the sign of a piece's channels
-template <typename T> __device__ __forceinline__ u32x4_t turn_sign(u32x4_t v, uint32_t sign) {
-    const uint32_t s = sizeof(T) == 2 ? sign | (sign >> 16) : sign;
-    return v ^ s;
 }
 
 // the same for tiles of 16 rows (lane = column lane % 16; sixteenth of the wavefront g = lane / 16): a

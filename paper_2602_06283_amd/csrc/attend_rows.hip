@@ -74,9 +74,9 @@ __device__ __forceinline__ void attend_plain(const RowsArgs &a, int b, int h, in
                 kr.get(kf);
                 qr.get(qf);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) dot = fmaf(kf[e], __uint_as_float(__float_as_uint(qf[e]) ^ a.mods.sign), dot);
+                for (int e = 0; e < 8; ++e) dot = fmaf(kf[e], qf[e], dot);
             }
-            s = logit2(a.mods, dot, (float)(i - t), slope2);
+            s = logit2(a.mods, dot, (float)(i - t), slope2, 0.0f);
         }
         const float top_new = fmaxf(top, wave_max(s)), use = top_new == ninf ? 0.0f : top_new;
         const float p = row >= 0 ? exp2_fast(s - use) : 0.0f, alpha = exp2_fast(top - use);
@@ -180,9 +180,10 @@ template <int D, int PX> struct ValueProduct<float, D, PX> {
     }
 };
 
+template <bool V> struct BoolTag { static constexpr bool value = V; };
 constexpr float kTopSlack = 8.0f;
 
-template <typename T, int D, int PX>
+template <typename T, int D, int PX, bool GEN>
 __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_kernel(RowsArgs a) {
     using Tile = KvTile<T, D>;
     constexpr int KT = Tile::KT, CPR = Tile::CPR, NU = KT / 32, NG = KT / 16;
@@ -192,7 +193,7 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_ke
     __shared__ __align__(16) int s_absent0[4], s_absent1[4];     // sixteenths of a tile whose block is absent
     __shared__ int s_lo[4], s_hi[4];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hf = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5;
     // all workgroups of a KV head on one XCD where there are eight heads or more (its L2 then serves the
     // head's keys), long rows first
     const int bh = (int)blockIdx.x % a.BH, rest = (int)blockIdx.x / a.BH;
@@ -211,28 +212,38 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_ke
         row_span(a.mods, b, i, run.len(), a.map.max_n, lo, hi);
         const T *src = (const T *)a.q + query_at(a, b, h, m) * D;
 #pragma unroll
-        for (int ks = 0; ks < NKS; ++ks) q[ks] = turn_sign<T>(*(const u32x4_t *)((const char *)src + (2 * ks + hf) * 16), a.mods.sign);
+        for (int ks = 0; ks < NKS; ++ks) q[ks] = *(const u32x4_t *)((const char *)src + (2 * ks + hf) * 16);
     } else {
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks) q[ks] = 0;
     }
     const float slope2 = a.mods.slopes && valid ? a.mods.slopes[h * a.G + (m & (a.G - 1))] * kLog2e : 0.0f;
 
-    // ---- the keys any query of the workgroup sees
-    const bool sees = lo <= hi;
-    int lo_w = sees ? lo : 0x7fffffff, hi_w = sees ? hi : -1;
+    // ---- the keys any query of the workgroup sees: without documents, from the first row's first to the last
+    //      row's last
+    int k_lo, k_hi;
+    if (a.mods.doc_begin == nullptr) {
+        const int i0 = run.begin + ((qt * kRowsQueries) >> a.g_log2);
+        int unused;
+        row_span(a.mods, b, i0, run.len(), a.map.max_n, k_lo, unused);
+        row_span(a.mods, b, min(i0 + (kRowsQueries >> a.g_log2), run.len()) - 1, run.len(), a.map.max_n, unused, k_hi);
+    } else {
+        const bool sees = lo <= hi;
+        int lo_w = sees ? lo : 0x7fffffff, hi_w = sees ? hi : -1;
 #pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-        lo_w = min(lo_w, __shfl_xor(lo_w, o));
-        hi_w = max(hi_w, __shfl_xor(hi_w, o));
+        for (int o = 1; o < 32; o *= 2) {
+            lo_w = min(lo_w, __shfl_xor(lo_w, o));
+            hi_w = max(hi_w, __shfl_xor(hi_w, o));
+        }
+        if (lane == 0) {
+            s_lo[wave] = lo_w;
+            s_hi[wave] = hi_w;
+        }
+        __syncthreads();
+        k_lo = min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3]));
+        k_hi = max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3]));
     }
-    if (lane == 0) {
-        s_lo[wave] = lo_w;
-        s_hi[wave] = hi_w;
-    }
-    __syncthreads();
-    const int k_lo = min(min(s_lo[0], s_lo[1]), min(s_lo[2], s_lo[3]));
-    const int k_hi = __builtin_amdgcn_readfirstlane(max(max(s_hi[0], s_hi[1]), max(s_hi[2], s_hi[3])));
+    k_hi = __builtin_amdgcn_readfirstlane(k_hi);
     const int base = __builtin_amdgcn_readfirstlane(k_lo & ~15);
     const int n_tiles = k_hi >= 0 ? (k_hi - base) / KT + 1 : 0;
     const int per = (n_tiles + a.n_split - 1) / a.n_split;
@@ -251,25 +262,32 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_ke
 #pragma unroll
         for (int p = 0; p < LOADS; ++p) {
             const int row = (p * kRowsThreads + wave * 64) / CPR;
-            const int t = __builtin_amdgcn_readfirstlane(min(base + tile * KT + row, k_hi));
+            const int t = min(base + tile * KT + row, k_hi);
             blk[p] = scalar_load(&a.map.block_table[(int64_t)b * a.map.max_blocks + a.map.page_slot(t)]);
         }
     };
-    auto load = [&](int tile, char *kt, char *vt, int *absent) __attribute__((always_inline)) {
+    auto load_as = [&](int tile, char *kt, char *vt, int *absent, auto whole) __attribute__((always_inline)) {
+        constexpr bool full = decltype(whole)::value;            // no row of the tile is behind the last key
 #pragma unroll
         for (int p = 0; p < LOADS; ++p) {
             const int slot = p * kRowsThreads + wave * 64, row0 = slot / CPR;        // the wavefront's first piece and row
             const int row = (slot + lane) / CPR, c = lane % CPR;
-            const int first = __builtin_amdgcn_readfirstlane(min((base + tile * KT + row0) & ~15, k_hi & ~15));
+            const int sixteen = base + tile * KT + (row0 & ~15);
+            const int first = full ? sixteen : min(sixteen, k_hi & ~15);
             const bool gone = (unsigned)blk[p] >= (unsigned)rows.blocks;
             const int64_t at = rows.at(gone ? 0 : blk[p], first);
             if ((row0 & 15) == 0 && lane == 0) absent[row0 >> 4] = gone;
-            const int in = min(base + tile * KT + row, k_hi) - first;                // (rows behind the last key read it again)
+            // (rows behind the last key read it again)
             const char *ks = (const char *)a.K + at * Tile::ROWB, *vs = (const char *)a.V + at * Tile::ROWB;
-            const uint32_t k_off = (uint32_t)(in * Tile::ROWB + Tile::k_turned(row, c) * 16), v_off = (uint32_t)(in * Tile::ROWB + Tile::v_turned(row, c) * 16);
+            const uint32_t in = (uint32_t)(full ? row & 15 : min(base + tile * KT + row, k_hi) - first) * Tile::ROWB;
+            const uint32_t k_off = in + Tile::k_turned(row, c) * 16, v_off = in + Tile::v_turned(row, c) * 16;
             lds_fill(ks + k_off, kt + slot * 16);
             lds_fill(vs + v_off, vt + slot * 16);
         }
+    };
+    auto load = [&](int tile, char *kt, char *vt, int *absent) __attribute__((always_inline)) {
+        if (base + tile * KT + KT - 1 <= k_hi) load_as(tile, kt, vt, absent, BoolTag<true>());
+        else load_as(tile, kt, vt, absent, BoolTag<false>());
     };
 
     floatx16_t o[D / 32];
@@ -302,13 +320,11 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_ke
 #pragma unroll
                     for (int r = 0; r < 16; ++r) s[u][r] = c[u][r];
             }
-            float cc = a.mods.c;
-            if (a.mods.general) {
+            // ... less what the weights are taken against
+            const float ref = top == ninf ? 0.0f : top;
 #pragma unroll
-                for (int u = 0; u < NU; ++u)
-                    logits2(a.mods, s[u], (float)(i - t0 - 32 * u), slope2, [&](int r) { return tile_row(r, hf); });
-                cc = 1.0f;
-            }
+            for (int u = 0; u < NU; ++u)
+                logits2<GEN>(a.mods, s[u], (float)(i - t0 - 32 * u), slope2, ref, [&](int r) { return tile_row(r, hf); });
             // ---- masks
             int gone = 0;
             if (a.map.block_table) {
@@ -329,7 +345,8 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_ke
                     }
                 }
             }
-            // ---- running maximum, weights and their sum
+            // ---- running maximum, weights and their sum.  What the weights are taken against need not be the
+            //      maximum itself: it stays, and the sums with it, until one is above 2^8.
             float mx = s[0][0];
 #pragma unroll
             for (int u = 0; u < NU; ++u)
@@ -339,24 +356,24 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_ke
                 auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
                 mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
             }
-            mx = mx == ninf ? ninf : mx * cc;
-            // (what the weights are taken against need not be the maximum itself: as long as none is above
-            // 2^8 it stays, and the sums with it)
-            if (__any(mx > top + kTopSlack)) {
-                const float top_new = fmaxf(top, mx);
-                const float alpha = top_new == ninf ? 1.0f : exp2_fast(top - top_new);
+            const bool raise = mx > kTopSlack || (top == ninf && mx > ninf);
+            if (__any(raise)) {
+                const float by = raise ? mx : 0.0f, alpha = top == ninf ? 1.0f : exp2_fast(-by);   // (nothing yet: nothing to scale)
+                if (raise) top = ref + by;
                 sum *= alpha;
 #pragma unroll
                 for (int cb = 0; cb < D / 32; ++cb) o[cb] *= alpha;
-                top = top_new;
+#pragma unroll
+                for (int u = 0; u < NU; ++u)
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) s[u][r] -= by;
             }
-            const float use = top == ninf ? 0.0f : top;
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
                 float part = 0.0f;
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
-                    s[u][r] = exp2_fast(fmaf(s[u][r], cc, -use));
+                    s[u][r] = exp2_fast(s[u][r]);
                     part += s[u][r];
                 }
                 sum += part;
@@ -469,7 +486,7 @@ __global__ __launch_bounds__(64) void attend_few_kernel(RowsArgs a) {
             row_span(a.mods, b, run.begin + (m >> a.g_log2), run.len(), a.map.max_n, lo[x], hi[x]);
             const char *src = (const char *)a.q + query_at(a, b, h, m) * Tile::ROWB;
 #pragma unroll
-            for (int ks = 0; ks < NKS; ++ks) q[x][ks] = turn_sign<T>(*(const u32x4_t *)(src + (4 * ks + g) * 16), a.mods.sign);
+            for (int ks = 0; ks < NKS; ++ks) q[x][ks] = *(const u32x4_t *)(src + (4 * ks + g) * 16);
             if (a.mods.slopes) slope2[x] = a.mods.slopes[h * a.G + (m & (a.G - 1))] * kLog2e;
             if (lo[x] <= hi[x]) {
                 lo_w = min(lo_w, lo[x]);
@@ -479,26 +496,23 @@ __global__ __launch_bounds__(64) void attend_few_kernel(RowsArgs a) {
     }
     // the longest span of the batch decides how many keys a split takes: the same for all sequences, so that
     // those of a long one are not behind at the end
-    int longest = 0;
-    for (int y = lane; y < a.batch; y += 64) {
-        const int begin = a.row_begin[y], count = min(a.row_count[y], a.max_rows);
-        if (begin >= 0 && begin < a.map.max_n && count > 0) {
-            int span = min(begin + count, a.map.max_n);
-            if (a.mods.window > 0 && a.mods.window < span) span = min(span, a.mods.window + count - 1);
-            longest = max(longest, span);
-        }
-    }
+    int longest = a.mods.window > 0 && a.mods.window < run.len() ? min(run.len(), a.mods.window + run.count - 1) : run.len();
+    if (a.batch > 1) longest = longest_of(a.row_begin, a.row_count, a.batch, a.max_rows, a.map.max_n, a.mods.window);
+    int k_lo = a.mods.window > 0 ? max(0, run.begin - a.mods.window + 1) : 0, k_hi = run.len() - 1;
+    if (a.mods.doc_begin) {
 #pragma unroll
-    for (int o = 1; o < 64; o *= 2) {
-        lo_w = min(lo_w, __shfl_xor(lo_w, o));
-        hi_w = max(hi_w, __shfl_xor(hi_w, o));
-        longest = max(longest, __shfl_xor(longest, o));
+        for (int o = 1; o < 16; o *= 2) {
+            lo_w = min(lo_w, __shfl_xor(lo_w, o));
+            hi_w = max(hi_w, __shfl_xor(hi_w, o));
+        }
+        k_lo = lo_w;
+        k_hi = hi_w;
     }
-    const int k_hi = __builtin_amdgcn_readfirstlane(hi_w);
-    const int base = __builtin_amdgcn_readfirstlane(lo_w & ~15);
+    k_hi = __builtin_amdgcn_readfirstlane(k_hi);
+    const int base = __builtin_amdgcn_readfirstlane(k_lo & ~15);
     const int n_tiles = k_hi >= 0 ? (k_hi - base) / KT + 1 : 0;
     const int share = ((longest + 15 + KT - 1) / KT + a.n_split - 1) / a.n_split;
-    const int per = __builtin_amdgcn_readfirstlane(max(share, 64 / KT));
+    const int per = __builtin_amdgcn_readfirstlane(max(share, 1));
     const int t_begin = min(n_tiles, split * per), t_end = min(n_tiles, t_begin + per);
 
     // ---- rows of a tile, sixteen by sixteen (a block holds whole sixteens)
@@ -585,12 +599,9 @@ __global__ __launch_bounds__(64) void attend_few_kernel(RowsArgs a) {
         }
 #pragma unroll
         for (int x = 0; x < NQ; ++x) {
-            float cc = a.mods.c;
-            if (a.mods.general) {
-                const int i = run.begin + ((16 * x + (lane & 15)) >> a.g_log2);
-                logits2(a.mods, s[x], (float)(i - t0), slope2[x], [&](int e) { return 16 * (e / 4) + 4 * g + e % 4; });
-                cc = 1.0f;
-            }
+            const float ref = top[x] == ninf ? 0.0f : top[x];
+            logits2<true>(a.mods, s[x], (float)(run.begin + ((16 * x + (lane & 15)) >> a.g_log2) - t0), slope2[x], ref,
+                    [&](int e) { return 16 * (e / 4) + 4 * g + e % 4; });
             if (__any(lo[x] > t0 || hi[x] < t0 + KT - 1) || gone) {
                 const uint32_t span = (uint32_t)(hi[x] - lo[x]);
                 const bool any = lo[x] <= hi[x];
@@ -604,19 +615,20 @@ __global__ __launch_bounds__(64) void attend_few_kernel(RowsArgs a) {
 #pragma unroll
             for (int e = 1; e < 4 * NT; ++e) mx = fmaxf(mx, s[x][e]);
             mx = sixteenths_max(mx);
-            const float top_new = fmaxf(top[x], mx == ninf ? ninf : mx * cc);
-            const float use = top_new == ninf ? 0.0f : top_new;
-            if (__any(top_new > top[x])) {
-                const float alpha = exp2_fast(top[x] - use);
+            const bool raise = mx > kTopSlack || (top[x] == ninf && mx > ninf);
+            if (__any(raise)) {
+                const float by = raise ? mx : 0.0f, alpha = top[x] == ninf ? 1.0f : exp2_fast(-by);
+                if (raise) top[x] = ref + by;
                 sum[x] *= alpha;
 #pragma unroll
                 for (int cb = 0; cb < NCB; ++cb) o[x][cb] *= alpha;
+#pragma unroll
+                for (int e = 0; e < 4 * NT; ++e) s[x][e] -= by;
             }
-            top[x] = top_new;
             float part = 0.0f;
 #pragma unroll
             for (int e = 0; e < 4 * NT; ++e) {
-                s[x][e] = exp2_fast(fmaf(s[x][e], cc, -use));
+                s[x][e] = exp2_fast(s[x][e]);
                 part += s[x][e];
             }
             sum[x] += part;
@@ -708,27 +720,40 @@ __global__ __launch_bounds__(64) void attend_few_kernel(RowsArgs a) {
     }
 }
 
-// Joins the splits of one query: out = sum_s w_s acc_s / sum_s w_s l_s, w_s = exp2(m_s - max m).
-constexpr int kRowsMergeThreads = 256;
+// Joins the splits of one query: out = sum_s w_s acc_s / sum_s w_s l_s, w_s = exp2(m_s - max m), by channel
+// pairs; a group of threads takes every NG-th split.  Bound by latency: all loads go out before the first is
+// used (one after the other, 128 splits of 32 query heads took 17 us).
+constexpr int kRowsMergeThreads = 512;
 template <int D>
 __global__ __launch_bounds__(kRowsMergeThreads) void attend_rows_merge_kernel(RowsArgs a) {
-    constexpr int NG = kRowsMergeThreads / D;
-    __shared__ float s_w[kMaxSplits], s_red[kRowsMergeThreads], s_sum, s_top;
-    const int tid = threadIdx.x, c = tid % D, grp = tid / D;
+    constexpr int PAIRS = D / 2, NG = kRowsMergeThreads / PAIRS, BATCH = 8, NB = kMaxSplits / (NG * BATCH);
+    __shared__ float s_w[kMaxSplits], s_sum, s_top;
+    __shared__ float2 s_red[kRowsMergeThreads];
+    const int tid = threadIdx.x, c = tid % PAIRS, grp = tid / PAIRS;
     const int hq = blockIdx.x, r = blockIdx.y, b = blockIdx.z;
-    const RowRun run(a.row_begin, a.row_count, b, a.max_rows, a.map.max_n);
-    if (r >= run.count) return;
     const int64_t at = ((int64_t)b * a.max_rows + r) * a.Hq + hq;
     const float *part = a.partials + at * a.n_split * (D + 2);
     const float ninf = -__builtin_inff();
-    if (tid < 64) {
-        float m[2], l[2];
+    float m[2], l[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int s = tid + 64 * j;
-            m[j] = s < a.n_split ? part[(int64_t)s * (D + 2)] : ninf;
-            l[j] = s < a.n_split ? part[(int64_t)s * (D + 2) + 1] : 0.0f;
+    for (int j = 0; j < 2; ++j) {
+        const int s = tid + 64 * j;
+        const bool live = tid < 64 && s < a.n_split;
+        const float2 ml = live ? *(const float2 *)&part[(int64_t)s * (D + 2)] : make_float2(ninf, 0.0f);
+        m[j] = ml.x;
+        l[j] = ml.y;
+    }
+    float2 x[NB][BATCH];
+#pragma unroll
+    for (int y = 0; y < NB; ++y) {
+        if (y * BATCH * NG < a.n_split) {
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) x[y][j] = *(const float2 *)&part[(int64_t)min((y * BATCH + j) * NG + grp, a.n_split - 1) * (D + 2) + 2 + 2 * c];
         }
+    }
+    const RowRun run(a.row_begin, a.row_count, b, a.max_rows, a.map.max_n);
+    if (r >= run.count) return;                      // (what was read is not used)
+    if (tid < 64) {
         const float top = wave_max(fmaxf(m[0], m[1])), use = top == ninf ? 0.0f : top;
         const float w0 = exp2_fast(m[0] - use), w1 = exp2_fast(m[1] - use);
         const float sum = row_sum<64>(w0 * l[0] + w1 * l[1]);
@@ -740,32 +765,48 @@ __global__ __launch_bounds__(kRowsMergeThreads) void attend_rows_merge_kernel(Ro
         }
     }
     __syncthreads();
-    float acc = 0.0f;
-    for (int s = grp; s < a.n_split; s += NG) {
-        const float w = s_w[s];
-        const float x = part[(int64_t)s * (D + 2) + 2 + c];
-        if (w > 0.0f || w != w) acc = fmaf(w, x, acc);           // (an empty split's values are zeros)
+    float2 acc = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int y = 0; y < NB; ++y) {
+        if (y * BATCH * NG < a.n_split) {
+#pragma unroll
+            for (int j = 0; j < BATCH; ++j) {
+                const int s = (y * BATCH + j) * NG + grp;
+                const float w = s < a.n_split ? s_w[s] : 0.0f;
+                // (a split without keys has written no values)
+                acc.x = w != 0.0f ? fmaf(w, x[y][j].x, acc.x) : acc.x;
+                acc.y = w != 0.0f ? fmaf(w, x[y][j].y, acc.y) : acc.y;
+            }
+        }
     }
     s_red[tid] = acc;
     __syncthreads();
     if (grp == 0) {
 #pragma unroll
-        for (int k = 1; k < NG; ++k) acc += s_red[k * D + c];
-        const float sum = s_sum, y = sum == 0.0f ? 0.0f : acc / sum;
-        if (a.out_dtype == SOCKET_F32) ((float *)a.out)[at * D + c] = y;
-        else ((uint16_t *)a.out)[at * D + c] = f32_to_bf16_rne(y);
+        for (int k = 1; k < NG; ++k) {
+            const float2 v = s_red[k * PAIRS + c];
+            acc.x += v.x;
+            acc.y += v.y;
+        }
+        const float sum = s_sum, y0 = sum == 0.0f ? 0.0f : acc.x / sum, y1 = sum == 0.0f ? 0.0f : acc.y / sum;
+        if (a.out_dtype == SOCKET_F32) *(float2 *)((float *)a.out + at * D + 2 * c) = make_float2(y0, y1);
+        else *(uint32_t *)((uint16_t *)a.out + at * D + 2 * c) = pack_bf16(y0, y1);
         if (a.lse && c == 0) a.lse[at] = sum == 0.0f ? ninf : (s_top + __builtin_amdgcn_logf(sum)) * kLn2;
     }
 }
 
-template <typename T, int D> static void launch_rows(const RowsArgs &a, dim3 grid, hipStream_t st) {
+template <typename T, int D, bool GEN> static void launch_rows(const RowsArgs &a, dim3 grid, hipStream_t st) {
     if constexpr (sizeof(T) == 2) {
         if (a.out_dtype == SOCKET_F32) {
-            hipLaunchKernelGGL((attend_rows_kernel<T, D, 3>), grid, dim3(kRowsThreads), 0, st, a);
+            hipLaunchKernelGGL((attend_rows_kernel<T, D, 3, GEN>), grid, dim3(kRowsThreads), 0, st, a);
             return;
         }
     }
-    hipLaunchKernelGGL((attend_rows_kernel<T, D, 1>), grid, dim3(kRowsThreads), 0, st, a);
+    hipLaunchKernelGGL((attend_rows_kernel<T, D, 1, GEN>), grid, dim3(kRowsThreads), 0, st, a);
+}
+template <typename T, int D> static void launch_rows(const RowsArgs &a, dim3 grid, hipStream_t st) {
+    if (a.mods.a > 0.0f || a.mods.slopes) launch_rows<T, D, true>(a, grid, st);
+    else launch_rows<T, D, false>(a, grid, st);
 }
 
 template <typename T, int D> static void launch_few(const RowsArgs &a, bool wide, dim3 grid, hipStream_t st) {
@@ -804,10 +845,10 @@ int launch_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void
     const int64_t room = ctx->partial_floats / ((int64_t)batch * max_rows * g.Hq * (g.d + 2));   // splits whose results fit
     const bool f32 = g.kv_dtype == SOCKET_F32;
     if ((int64_t)max_rows * g.G <= 32) {
-        // One wavefront a split, at least 64 keys each: with 16 and more of them to a compute unit the last
+        // One wavefront a split, at least a tile of keys each: with 16 and more of them to a compute unit the last
         // ones to finish are a small part.
         a.n_tiles = 1;
-        a.n_split = pick_splits(8192 / a.BH, (g.max_n + 63) / 64, room);
+        a.n_split = pick_splits(8192 / a.BH, (g.max_n + 31) / 32, room);
         const int64_t grid = (int64_t)a.BH * a.n_split;
         if (grid >= (int64_t)1 << 31) return SOCKET_EUNSUPPORTED;
         const dim3 gr((unsigned)grid);

@@ -65,7 +65,7 @@ __global__ __launch_bounds__(kMassThreads, D <= 128 ? 2 : 1) void key_mass_kerne
     __shared__ __align__(16) char s_q0[Tile::BYTES], s_q1[Tile::BYTES];
     __shared__ MassMeta s_meta0, s_meta1;
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, hf = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5;
     const int bh = (int)blockIdx.x % a.BH, rest = (int)blockIdx.x / a.BH;
     const int seg = rest % a.n_seg, kb = rest / a.n_seg;
     const int b = bh / a.map.Hkv, h = bh - b * a.map.Hkv;
@@ -158,22 +158,18 @@ __global__ __launch_bounds__(kMassThreads, D <= 128 ? 2 : 1) void key_mass_kerne
                 const int v0 = w0 + 32 * y;
                 float s[16];
 #pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = a.mods.sign ? -c[y][r] : c[y][r];
-                float cc = a.mods.c;
-                if (a.mods.general) {
-                    logits2(a.mods, s, (float)(meta.i[n] - v0), meta.slope[n], [&](int r) { return tile_row(r, hf); });
-                    cc = 1.0f;
-                }
+                for (int r = 0; r < 16; ++r) s[r] = c[y][r];
+                logits2<true>(a.mods, s, (float)(meta.i[n] - v0), meta.slope[n], lse, [&](int r) { return tile_row(r, hf); });
                 if (__all(lo <= v0 && hi >= v0 + 31) && there[y] == 0xffffffffu) {
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[y][r] += exp2_fast(fmaf(s[r], cc, -lse));
+                    for (int r = 0; r < 16; ++r) acc[y][r] += exp2_fast(s[r]);
                 } else {
                     const uint32_t span = (uint32_t)(hi - lo);
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
                         const int row = tile_row(r, hf);
                         const bool vis = lo <= hi && (uint32_t)(v0 + row - lo) <= span && ((there[y] >> row) & 1u);
-                        const float p = exp2_fast(fmaf(s[r], cc, -lse));
+                        const float p = exp2_fast(s[r]);
                         acc[y][r] += vis ? p : 0.0f;
                     }
                 }
@@ -243,13 +239,7 @@ __global__ __launch_bounds__(64) void key_mass_few_kernel(MassArgs a) {
     if (run.count == 0) return;
     const int len = run.len();
     // the same number of keys for every wavefront of the batch
-    int longest = 0;
-    for (int y = lane; y < a.batch; y += 64) {
-        const int begin = a.row_begin[y], count = min(a.row_count[y], a.max_rows);
-        if (begin >= 0 && begin < a.map.max_n && count > 0) longest = max(longest, min(begin + count, a.map.max_n));
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o *= 2) longest = max(longest, __shfl_xor(longest, o));
+    const int longest = a.batch > 1 ? longest_of(a.row_begin, a.row_count, a.batch, a.max_rows, a.map.max_n, 0) : len;
     const int per = __builtin_amdgcn_readfirstlane(max(((longest + KT - 1) / KT + a.n_seg - 1) / a.n_seg, 64 / KT));
     const int n_tiles = (len + KT - 1) / KT, t_begin = share_at * per, t_end = min(n_tiles, t_begin + per);
     if (t_begin >= t_end) return;
@@ -307,7 +297,7 @@ __global__ __launch_bounds__(64) void key_mass_few_kernel(MassArgs a) {
             lse[x] = a.lse[at] * kLog2e;
             if (lse[x] == -__builtin_inff()) hi[x] = -1;
 #pragma unroll
-            for (int ks = 0; ks < NKS; ++ks) q[x][ks] = turn_sign<T>(*(const u32x4_t *)((const char *)a.q + at * ROWB + (4 * ks + g) * 16), a.mods.sign);
+            for (int ks = 0; ks < NKS; ++ks) q[x][ks] = *(const u32x4_t *)((const char *)a.q + at * ROWB + (4 * ks + g) * 16);
             if (a.mods.slopes) slope2[x] = a.mods.slopes[h * a.G + (m & (a.G - 1))] * kLog2e;
         }
     }
@@ -337,17 +327,13 @@ __global__ __launch_bounds__(64) void key_mass_few_kernel(MassArgs a) {
             float s[4 * NT];
 #pragma unroll
             for (int e = 0; e < 4 * NT; ++e) s[e] = c[x][e / 4][e % 4];
-            float cc = a.mods.c;
-            if (a.mods.general) {
-                const int i = run.begin + ((first_m + 16 * x + (lane & 15)) >> a.g_log2);
-                logits2(a.mods, s, (float)(i - t0), slope2[x], [&](int e) { return 16 * (e / 4) + 4 * g + e % 4; });
-                cc = 1.0f;
-            }
+            logits2<true>(a.mods, s, (float)(run.begin + ((first_m + 16 * x + (lane & 15)) >> a.g_log2) - t0), slope2[x], lse[x],
+                    [&](int e) { return 16 * (e / 4) + 4 * g + e % 4; });
             const uint32_t span = (uint32_t)(hi[x] - lo[x]);
 #pragma unroll
             for (int e = 0; e < 4 * NT; ++e) {
                 const bool vis = lo[x] <= hi[x] && (uint32_t)(t0 + 16 * (e / 4) + 4 * g + e % 4 - lo[x]) <= span && !((gone >> (e / 4)) & 1);
-                const float p = exp2_fast(fmaf(s[e], cc, -lse[x]));
+                const float p = exp2_fast(s[e]);
                 sum[e] += vis ? p : 0.0f;
             }
         }
