@@ -87,10 +87,10 @@ __device__ __forceinline__ float logit2(const RowMods &m, float x, float dist, f
 
 // The same for the N dot products of one query that a lane holds of a tile, the key of x[n] being
 // key0 + row_of(n): capped logits are mostly far below the cap, so a wavefront whose arguments all are
-// small takes the ratio alone.  GEN: capped or biased.
-template <bool GEN, int N, typename F>
+// small takes the ratio alone.
+template <int N, typename F>
 __device__ __forceinline__ void logits2(const RowMods &m, float (&x)[N], float i_minus_key0, float slope2, float ref, F row_of) {
-    if (GEN && m.a > 0.0f) {
+    if (m.a > 0.0f) {
         float top = 0.0f;
 #pragma unroll
         for (int n = 0; n < N; ++n) {
@@ -108,11 +108,29 @@ __device__ __forceinline__ void logits2(const RowMods &m, float (&x)[N], float i
 #pragma unroll
         for (int n = 0; n < N; ++n) x[n] = fmaf(x[n], m.c, -ref);
     }
-    if (GEN && m.slopes) {
+    if (m.slopes) {
 #pragma unroll
         for (int n = 0; n < N; ++n) x[n] = fmaf(-slope2, fabsf(i_minus_key0 - (float)row_of(n)), x[n]);
     }
 }
+
+// The same one by one, for a kernel of its own per kind of logit.
+template <bool CAP, bool BIAS> struct LogitOf {
+    float c, a, ref, slope2, dist0;
+    __device__ __forceinline__ LogitOf(const RowMods &m, float i_minus_key0, float slope, float r)
+        : c(CAP ? m.y_scale : m.c), a(m.a), ref(r), slope2(slope), dist0(i_minus_key0) {}
+    __device__ __forceinline__ float biased(float s, int row) const { return BIAS ? fmaf(-slope2, fabsf(dist0 - (float)row), s) : s; }
+    // capped: right where |y| <= 1/4; `most` becomes the largest |y| so far
+    __device__ __forceinline__ float small(float x, int row, float &most) const {
+        if (!CAP) return biased(fmaf(x, c, -ref), row);
+        const float y = x * c;
+        most = fmaxf(most, fabsf(y));
+        return biased(fmaf(y * a, tanh_ratio(y * y), -ref), row);
+    }
+    __device__ __forceinline__ float any(float x, int row) const {
+        return biased(CAP ? fmaf(a, tanh_any(x * c), -ref) : fmaf(x, c, -ref), row);
+    }
+};
 
 // Longest sequence of a batch, cut to what a window lets its rows see: by one wavefront.
 __device__ __forceinline__ int longest_of(const int32_t *row_begin, const int32_t *row_count, int batch, int max_rows, int max_n, int window) {

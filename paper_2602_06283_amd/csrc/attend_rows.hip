@@ -128,63 +128,78 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(floatx2_t{lo, hi}, bf16x2_t));
 }
 
-// O^T += V^T P^T over the 32 keys of sub-tile u; p: the weights as the logits' tile left them
-template <typename T, int D, int PX> struct ValueProduct;
-template <int D, int PX> struct ValueProduct<uint16_t, D, PX> {
-    static __device__ __forceinline__ void run(floatx16_t (&o)[D / 32], const char *v, int u, float (&p)[16], int lane) {
-        using Tile = KvTile<uint16_t, D>;
-        const int hf = lane >> 5;
+// The value product O^T += V^T P^T of a tile, in stages: what a stage reads of V, and its matrix instructions.
+// w: the weights as it takes them, bf16 in PX pieces, or fp32.
+template <typename T, int D, int PX> struct ValueStages;
+template <int D, int PX> struct ValueStages<uint16_t, D, PX> {
+    using Tile = KvTile<uint16_t, D>;
+    static constexpr int NU = Tile::KT / 32, COUNT = NU * 2 * (D / 64);      // two blocks of 32 channels each
+    struct Part { u32x4_t v[2]; };
+    u32x4_t w[NU][2][PX];
+    // elements e, e + 1 of the tile's 16 NU (e even)
+    __device__ __forceinline__ void set(int e, float p0, float p1) {
+        const int u = e / 16, ks = e % 16 / 8;
 #pragma unroll
-        for (int ks = 0; ks < 2; ++ks) {
-            u32x4_t w[PX];
-#pragma unroll
-            for (int x = 0; x < PX; ++x) {
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float &p0 = p[8 * ks + 2 * e], &p1 = p[8 * ks + 2 * e + 1];
-                    w[x][e] = pack_bf16(p0, p1);
-                    if (x + 1 < PX) {
-                        p0 -= __uint_as_float(w[x][e] << 16);
-                        p1 -= __uint_as_float(w[x][e] & 0xffff0000u);
-                    }
-                }
-            }
-            // rows 16 ks + 4 hf + 0..3 and + 8: the lane's sixteenth of the wavefront reads four rows of
-            // 16 channels, transposed
-            const int row = 32 * u + 16 * ks + 4 * hf + ((lane & 15) >> 2);
-            const int c0 = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), in = (lane & 1) * 8;
-#pragma unroll
-            for (int cb = 0; cb < D / 32; ++cb) {
-                union { shortx4_t h[2]; u32x4_t v; } f;
-                f.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(v + Tile::v_piece(row, c0 + 4 * cb) * 16 + in));
-                f.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(v + Tile::v_piece(row + 8, c0 + 4 * cb) * 16 + in));
-#pragma unroll
-                for (int x = 0; x < PX; ++x) mma_piece<uint16_t>(o[cb], f.v, w[x]);
+        for (int x = 0; x < PX; ++x) {
+            const uint32_t both = pack_bf16(p0, p1);
+            w[u][ks][x][e % 8 / 2] = both;
+            if (x + 1 < PX) {
+                p0 -= __uint_as_float(both << 16);
+                p1 -= __uint_as_float(both & 0xffff0000u);
             }
         }
     }
-};
-template <int D, int PX> struct ValueProduct<float, D, PX> {
-    static __device__ __forceinline__ void run(floatx16_t (&o)[D / 32], const char *v, int u, float (&p)[16], int lane) {
-        using Tile = KvTile<float, D>;
-        const int hf = lane >> 5, ch = lane & 31;
+    // rows 16 ks + 4 hf + 0..3 and + 8 of sub-tile u: a sixteenth of the wavefront reads four rows of 16 channels,
+    // transposed
+    static __device__ __forceinline__ Part read(const char *v, int stage, int lane) {
+        const int u = stage / (D / 32), ks = stage / (D / 64) % 2, cb0 = stage % (D / 64) * 2, hf = lane >> 5;
+        const int row = 32 * u + 16 * ks + 4 * hf + ((lane & 15) >> 2);
+        const int c0 = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), in = (lane & 1) * 8;
+        Part part;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const int row = 32 * u + tile_row(r, hf);
-#pragma unroll
-            for (int cb = 0; cb < D / 32; ++cb) {
-                const float x = *(const float *)(v + Tile::v_piece(row, 8 * cb + (ch >> 2)) * 16 + (ch & 3) * 4);
-                o[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[r], o[cb], 0, 0, 0);
-            }
+        for (int y = 0; y < 2; ++y) {
+            union { shortx4_t h[2]; u32x4_t v; } f;
+            f.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(v + Tile::v_piece(row, c0 + 4 * (cb0 + y)) * 16 + in));
+            f.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(v + Tile::v_piece(row + 8, c0 + 4 * (cb0 + y)) * 16 + in));
+            part.v[y] = f.v;
         }
+        return part;
+    }
+    __device__ __forceinline__ void add(floatx16_t (&o)[D / 32], int stage, const Part &part) const {
+        const int u = stage / (D / 32), ks = stage / (D / 64) % 2, cb0 = stage % (D / 64) * 2;
+#pragma unroll
+        for (int x = 0; x < PX; ++x)
+#pragma unroll
+            for (int y = 0; y < 2; ++y) mma_piece<uint16_t>(o[cb0 + y], part.v[y], w[u][ks][x]);
+    }
+};
+template <int D, int PX> struct ValueStages<float, D, PX> {
+    using Tile = KvTile<float, D>;
+    static constexpr int NU = Tile::KT / 32, COUNT = 16 * NU;                // a register's rows each
+    struct Part { float v[D / 32]; };
+    float w[16 * NU];
+    __device__ __forceinline__ void set(int e, float p0, float p1) {
+        w[e] = p0;
+        w[e + 1] = p1;
+    }
+    static __device__ __forceinline__ Part read(const char *v, int stage, int lane) {
+        const int row = 32 * (stage / 16) + tile_row(stage % 16, lane >> 5), ch = lane & 31;
+        Part part;
+#pragma unroll
+        for (int cb = 0; cb < D / 32; ++cb) part.v[cb] = *(const float *)(v + Tile::v_piece(row, 8 * cb + (ch >> 2)) * 16 + (ch & 3) * 4);
+        return part;
+    }
+    __device__ __forceinline__ void add(floatx16_t (&o)[D / 32], int stage, const Part &part) const {
+#pragma unroll
+        for (int cb = 0; cb < D / 32; ++cb) o[cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(part.v[cb], w[stage], o[cb], 0, 0, 0);
     }
 };
 
 template <bool V> struct BoolTag { static constexpr bool value = V; };
 constexpr float kTopSlack = 8.0f;
 
-template <typename T, int D, int PX, bool GEN>
-__global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_kernel(RowsArgs a) {
+template <typename T, int D, int PX, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D <= 128 ? 2 : 1, D <= 128 ? 2 : 1))) void attend_rows_kernel(RowsArgs a) {
     using Tile = KvTile<T, D>;
     constexpr int KT = Tile::KT, CPR = Tile::CPR, NU = KT / 32, NG = KT / 16;
     constexpr int LOADS = KT * CPR / kRowsThreads;               // pieces of K (and of V) a thread brings
@@ -253,148 +268,220 @@ __global__ __launch_bounds__(kRowsThreads, D <= 128 ? 2 : 1) void attend_rows_ke
     //      turn of the pieces is done in the address it reads.  Its rows lie in one sixteenth of the cache
     //      (a block holds whole ones): one scalar look-up, made a tile ahead.  A buffer is an array of its own, and the
     //      loop goes over both: the compiler then sees that reads of one need not wait for the other's loads.
-    const BlockRows rows(a.map, b, h);
-    int blk[LOADS];
+    constexpr int RPL = kRowsThreads / CPR;          // rows that all wavefronts' loads of one turn cover
+    const bool paged = a.map.block_table != nullptr;
+    const int w_row = wave * 64 / CPR, l_row = lane / CPR, l_piece = lane % CPR;      // first row of the wavefront in a turn, row and piece of the lane
+    // the lane's byte in its wavefront's rows of a turn, and whether that is the same for every turn
+    constexpr bool ONE_TURN = RPL % 16 == 0;
+    auto byte_of = [&](int p, bool values) __attribute__((always_inline)) {
+        const int row = (p * RPL + w_row) % 16 + l_row;
+        return (uint32_t)(l_row * Tile::ROWB + (values ? Tile::v_turned(row, l_piece) : Tile::k_turned(row, l_piece)) * 16);
+    };
+    const uint32_t k_byte = byte_of(0, false), v_byte = byte_of(0, true);
+    const char *const k_head = (const char *)a.K + (paged ? (int64_t)h * a.map.page : (int64_t)bh * a.map.max_n + base) * Tile::ROWB;
+    const char *const v_head = (const char *)a.V + (paged ? (int64_t)h * a.map.page : (int64_t)bh * a.map.max_n + base) * Tile::ROWB;
+    const uint32_t block_bytes = (uint32_t)(a.map.Hkv * a.map.page * Tile::ROWB);
+    int blk_k[LOADS], blk_v[LOADS];
 #pragma unroll
-    for (int p = 0; p < LOADS; ++p) blk[p] = 0;
+    for (int p = 0; p < LOADS; ++p) blk_k[p] = blk_v[p] = 0;
     auto look_up = [&](int tile) __attribute__((always_inline)) {
-        if (a.map.block_table == nullptr || tile >= t_end) return;
+        if (!paged) return;
 #pragma unroll
         for (int p = 0; p < LOADS; ++p) {
-            const int row = (p * kRowsThreads + wave * 64) / CPR;
-            const int t = min(base + tile * KT + row, k_hi);
-            blk[p] = scalar_load(&a.map.block_table[(int64_t)b * a.map.max_blocks + a.map.page_slot(t)]);
+            blk_v[p] = blk_k[p];
+            if (tile >= t_end) continue;
+            blk_k[p] = scalar_load(&a.map.block_table[(int64_t)b * a.map.max_blocks + a.map.page_slot(min(base + tile * KT + p * RPL + w_row, k_hi))]);
         }
     };
-    auto load_as = [&](int tile, char *kt, char *vt, int *absent, auto whole) __attribute__((always_inline)) {
-        constexpr bool full = decltype(whole)::value;            // no row of the tile is behind the last key
+    auto load_rows = [&](int tile, const char *head, uint32_t byte, char *to, const int (&blk)[LOADS], auto is_v) __attribute__((always_inline)) {
+        constexpr bool VALUES = decltype(is_v)::value;
+        const int t0 = base + tile * KT;
+        // (one branch per tile for the form of the address: address arithmetic was a third of the instructions)
+        if (!paged && t0 + KT - 1 <= k_hi) {
+            const char *from = head + (int64_t)(tile * KT + w_row) * Tile::ROWB;
 #pragma unroll
-        for (int p = 0; p < LOADS; ++p) {
-            const int slot = p * kRowsThreads + wave * 64, row0 = slot / CPR;        // the wavefront's first piece and row
-            const int row = (slot + lane) / CPR, c = lane % CPR;
-            const int sixteen = base + tile * KT + (row0 & ~15);
-            const int first = full ? sixteen : min(sixteen, k_hi & ~15);
-            const bool gone = (unsigned)blk[p] >= (unsigned)rows.blocks;
-            const int64_t at = rows.at(gone ? 0 : blk[p], first);
-            if ((row0 & 15) == 0 && lane == 0) absent[row0 >> 4] = gone;
-            // (rows behind the last key read it again)
-            const char *ks = (const char *)a.K + at * Tile::ROWB, *vs = (const char *)a.V + at * Tile::ROWB;
-            const uint32_t in = (uint32_t)(full ? row & 15 : min(base + tile * KT + row, k_hi) - first) * Tile::ROWB;
-            const uint32_t k_off = in + Tile::k_turned(row, c) * 16, v_off = in + Tile::v_turned(row, c) * 16;
-            lds_fill(ks + k_off, kt + slot * 16);
-            lds_fill(vs + v_off, vt + slot * 16);
+            for (int p = 0; p < LOADS; ++p)
+                lds_fill(from + p * RPL * Tile::ROWB + (ONE_TURN ? byte : byte_of(p, VALUES)), to + (p * kRowsThreads + wave * 64) * 16);
+        } else {
+#pragma unroll
+            for (int p = 0; p < LOADS; ++p) {
+                // rows behind the last key read it again, sixteens behind it its own
+                const int first = min(t0 + p * RPL + w_row, k_hi);
+                const uint32_t in = (uint32_t)min(l_row, k_hi - first) * Tile::ROWB + (ONE_TURN ? byte : byte_of(p, VALUES)) - l_row * Tile::ROWB;
+                const bool gone = (unsigned)blk[p] >= (unsigned)(paged ? a.map.num_blocks : 1);
+                const char *from = head + (paged ? (uint64_t)(uint32_t)(gone ? 0 : blk[p]) * block_bytes + (int64_t)a.map.page_off(first) * Tile::ROWB
+                                                 : (uint64_t)(first - base) * Tile::ROWB);
+                lds_fill(from + in, to + (p * kRowsThreads + wave * 64) * 16);
+            }
         }
     };
-    auto load = [&](int tile, char *kt, char *vt, int *absent) __attribute__((always_inline)) {
-        if (base + tile * KT + KT - 1 <= k_hi) load_as(tile, kt, vt, absent, BoolTag<true>());
-        else load_as(tile, kt, vt, absent, BoolTag<false>());
+    auto load_k = [&](int tile, char *to, int *absent) __attribute__((always_inline)) {
+        if (paged) {
+#pragma unroll
+            for (int p = 0; p < LOADS; ++p)
+                if ((p * RPL + w_row) % 16 == 0 && lane == 0) absent[(p * RPL + w_row) / 16] = (unsigned)blk_k[p] >= (unsigned)a.map.num_blocks;
+        }
+        load_rows(tile, k_head, k_byte, to, blk_k, BoolTag<false>());
     };
+    auto load_v = [&](int tile, char *to) __attribute__((always_inline)) { load_rows(tile, v_head, v_byte, to, blk_v, BoolTag<true>()); };
 
     floatx16_t o[D / 32];
 #pragma unroll
     for (int cb = 0; cb < D / 32; ++cb) o[cb] = 0.0f;
     const float ninf = -__builtin_inff();
-    float top = ninf, sum = 0.0f;                    // running maximum and this lane's half of the running sum
+    // what the weights are taken against, and this lane's half of their sum.  It need not be the maximum
+    // itself: it stays, and the sums with it, until a logit is 2^8 above it.
+    float top = ninf, sum = 0.0f;
 
-    // one tile from (kt, vt), while the next one is on its way to (kn, vn)
-    auto tile_step = [&](int tile, const char *kt, const char *vt, const int *absent, char *kn, char *vn, int *absent_n) __attribute__((always_inline)) {
-        if (tile + 1 < t_end) {
-            load(tile + 1, kn, vn, absent_n);
-            look_up(tile + 2);
+    constexpr int E = 16 * NU;                       // logits a lane holds of a tile
+    // logit e of a lane is that of key 4 hf + key_row(e) of the tile.  (The lane's part apart, so that nothing but
+    // constants differs between the logits: their sums with it were kept in registers otherwise, one each.)
+    auto key_row = [](int e) __attribute__((always_inline)) { return 32 * (e / 16) + tile_row(e % 16, 0); };
+    const int i_lane = i - 4 * hf - base;
+    auto read_k = [&](const char *kt, int ks, u32x4_t (&f)[NU]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < NU; ++u) f[u] = *(const u32x4_t *)(kt + Tile::k_piece(32 * u + (lane & 31), 2 * ks + hf) * 16);
+    };
+    auto products = [&](const char *kt, floatx16_t (&s)[NU]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int u = 0; u < NU; ++u) s[u] = 0.0f;
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) {
+            u32x4_t f[NU];
+            read_k(kt, ks, f);
+#pragma unroll
+            for (int u = 0; u < NU; ++u) mma_piece<T>(s[u], f[u], q[ks]);
         }
+    };
+    auto across = [&](float x) __attribute__((always_inline)) {              // the larger of the two halves'
+        auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+    };
+    auto largest = [&](const floatx16_t (&s)[NU]) __attribute__((always_inline)) {
+        float mx = s[0][0];
+#pragma unroll
+        for (int e = 1; e < E; ++e) mx = fmaxf(mx, s[e / 16][e % 16]);
+        return across(mx);
+    };
+    // masks, and `top` raised where a logit asks for it
+    auto settle = [&](int tile, floatx16_t (&s)[NU], float mx, const int *absent) __attribute__((always_inline)) {
         const int t0 = base + tile * KT;
-        if (__any(valid && lo <= t0 + KT - 1 && hi >= t0)) {
-            // ---- logits
-            float s[NU][16];
-            {
-                floatx16_t c[NU];
+        int gone = 0;
+        if (a.map.block_table) {
 #pragma unroll
-                for (int u = 0; u < NU; ++u) c[u] = 0.0f;
-#pragma unroll
-                for (int ks = 0; ks < NKS; ++ks)
-#pragma unroll
-                    for (int u = 0; u < NU; ++u)
-                        mma_piece<T>(c[u], *(const u32x4_t *)(kt + Tile::k_piece(32 * u + (lane & 31), 2 * ks + hf) * 16), q[ks]);
-#pragma unroll
-                for (int u = 0; u < NU; ++u)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[u][r] = c[u][r];
-            }
-            // ... less what the weights are taken against
-            const float ref = top == ninf ? 0.0f : top;
-#pragma unroll
-            for (int u = 0; u < NU; ++u)
-                logits2<GEN>(a.mods, s[u], (float)(i - t0 - 32 * u), slope2, ref, [&](int r) { return tile_row(r, hf); });
-            // ---- masks
-            int gone = 0;
-            if (a.map.block_table) {
-#pragma unroll
-                for (int g = 0; g < NG; ++g) gone |= absent[g] << g;
-                gone = __builtin_amdgcn_readfirstlane(gone);
-            }
-            if (__any(valid && (lo > t0 || hi < t0 + KT - 1)) || gone) {
-                const uint32_t span = (uint32_t)(hi - lo);
-                const bool any = lo <= hi;
-#pragma unroll
-                for (int u = 0; u < NU; ++u) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int row = 32 * u + tile_row(r, hf);
-                        const bool vis = any && (uint32_t)(t0 + row - lo) <= span && !((gone >> (2 * u + r / 8)) & 1);
-                        s[u][r] = vis ? s[u][r] : ninf;
-                    }
-                }
-            }
-            // ---- running maximum, weights and their sum.  What the weights are taken against need not be the
-            //      maximum itself: it stays, and the sums with it, until one is above 2^8.
-            float mx = s[0][0];
-#pragma unroll
-            for (int u = 0; u < NU; ++u)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[u][r]);
-            {
-                auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
-                mx = fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-            }
-            const bool raise = mx > kTopSlack || (top == ninf && mx > ninf);
-            if (__any(raise)) {
-                const float by = raise ? mx : 0.0f, alpha = top == ninf ? 1.0f : exp2_fast(-by);   // (nothing yet: nothing to scale)
-                if (raise) top = ref + by;
-                sum *= alpha;
-#pragma unroll
-                for (int cb = 0; cb < D / 32; ++cb) o[cb] *= alpha;
-#pragma unroll
-                for (int u = 0; u < NU; ++u)
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) s[u][r] -= by;
-            }
-#pragma unroll
-            for (int u = 0; u < NU; ++u) {
-                float part = 0.0f;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    s[u][r] = exp2_fast(s[u][r]);
-                    part += s[u][r];
-                }
-                sum += part;
-            }
-            // ---- values
-#pragma unroll
-            for (int u = 0; u < NU; ++u) ValueProduct<T, D, PX>::run(o, vt, u, s[u], lane);
+            for (int g = 0; g < NG; ++g) gone |= absent[g] << g;
+            gone = __builtin_amdgcn_readfirstlane(gone);
         }
-        __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): this wavefront's part of the next tile is there
+        if (__any(valid && (lo > t0 || hi < t0 + KT - 1)) || gone) {
+            // (a row that sees nothing: every difference is negative, and so above the span 0)
+            const uint32_t span = lo <= hi ? (uint32_t)(hi - lo) : 0u;
+            int from = lo <= hi ? t0 + 4 * hf - lo : -0x40000000;
+            asm volatile("" : "+v"(from));           // (its sums belong here, not ahead of the branch)
+            if (gone == 0) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[e / 16][e % 16] = (uint32_t)(from + key_row(e)) <= span ? s[e / 16][e % 16] : ninf;
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[e / 16][e % 16] = (((uint32_t)(from + key_row(e)) <= span) & !((gone >> (e / 8)) & 1)) ? s[e / 16][e % 16] : ninf;
+            }
+            mx = largest(s);
+        }
+        const bool raise = mx > kTopSlack || (top == ninf && mx > ninf);
+        if (__any(raise)) {
+            const float by = raise ? mx : 0.0f, alpha = top == ninf ? 1.0f : exp2_fast(-by);   // (nothing yet: nothing to scale)
+            if (raise) top = (top == ninf ? 0.0f : top) + by;
+            sum *= alpha;
+#pragma unroll
+            for (int cb = 0; cb < D / 32; ++cb) o[cb] *= alpha;
+#pragma unroll
+            for (int e = 0; e < E; ++e) s[e / 16][e % 16] -= by;
+        }
+    };
+    // One tile, whose logits are there.  The exponentials run beside the products of the next tile's keys, its
+    // values beside the next tile's logits; the tile after that is on its way.  In stages of a few matrix instructions,
+    // whose operands are read from LDS two stages before (the compiler's own order reads each right before its
+    // use, and every matrix instruction waits for LDS) and the vector work of the softmax shared out among them.
+    auto tile_step = [&](int tile, floatx16_t (&s)[NU], const char *k_next, const char *v_now, const int *absent_next, char *k_to, char *v_to, int *absent_to) __attribute__((always_inline)) {
+        using Values = ValueStages<T, D, PX>;
+        constexpr int AHEAD = 2, RING = AHEAD + 1;
+        u32x4_t fk[RING][NU];
+        typename Values::Part fv[RING];
+        Values values;
+#pragma unroll
+        for (int ks = 0; ks < AHEAD; ++ks) read_k(k_next, ks, fk[ks]);
+        if (tile + 1 < t_end) load_v(tile + 1, v_to);
+        if (tile + 2 < t_end) load_k(tile + 2, k_to, absent_to);
+        look_up(tile + 3);
+        floatx16_t c[NU];                            // (behind the last tile: products of what the buffer holds, not used)
+#pragma unroll
+        for (int u = 0; u < NU; ++u) c[u] = 0.0f;
+        float part[2] = {0.0f, 0.0f};
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) {
+            if (ks + AHEAD < NKS) read_k(k_next, ks + AHEAD, fk[(ks + AHEAD) % RING]);
+            else fv[(ks + AHEAD - NKS) % RING] = Values::read(v_now, ks + AHEAD - NKS, lane);
+#pragma unroll
+            for (int u = 0; u < NU; ++u) mma_piece<T>(c[u], fk[ks % RING][u], q[ks]);
+#pragma unroll
+            for (int e = E * ks / NKS / 2 * 2; e < E * (ks + 1) / NKS / 2 * 2; e += 2) {
+                const float p0 = exp2_fast(s[e / 16][e % 16]), p1 = exp2_fast(s[e / 16][e % 16 + 1]);
+                part[0] += p0;
+                part[1] += p1;
+                values.set(e, p0, p1);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        sum += part[0] + part[1];
+        const float ref = top == ninf ? 0.0f : top;
+        const LogitOf<CAP, BIAS> logit(a.mods, (float)(i_lane - (tile + 1) * KT), slope2, ref);
+        float mx = ninf, most = 0.0f;
+#pragma unroll
+        for (int st = 0; st < Values::COUNT; ++st) {
+            if (st + AHEAD < Values::COUNT) fv[(st + AHEAD) % RING] = Values::read(v_now, st + AHEAD, lane);
+            values.add(o, st, fv[st % RING]);
+#pragma unroll
+            for (int e = E * st / Values::COUNT; e < E * (st + 1) / Values::COUNT; ++e) {
+                c[e / 16][e % 16] = logit.small(c[e / 16][e % 16], key_row(e), most);
+                mx = fmaxf(mx, c[e / 16][e % 16]);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (tile + 1 < t_end) {
+            mx = across(mx);
+            if (CAP && !__all(most <= kCapSmall)) {  // (also a NaN among them is no matter: the logit is one in either form)
+                products(k_next, c);
+#pragma unroll
+                for (int e = 0; e < E; ++e) c[e / 16][e % 16] = logit.any(c[e / 16][e % 16], key_row(e));
+                mx = largest(c);
+            }
+            settle(tile + 1, c, mx, absent_next);
+        }
+#pragma unroll
+        for (int u = 0; u < NU; ++u) s[u] = c[u];
+        __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): this wavefront's part of what comes next is there
         __syncthreads();
     };
     if (t_begin < t_end) {
+        floatx16_t s[NU];
         look_up(t_begin);
-        load(t_begin, s_k0, s_v0, s_absent0);
+        load_k(t_begin, s_k0, s_absent0);
         look_up(t_begin + 1);
-    }
-    __builtin_amdgcn_s_waitcnt(0x0f70);
-    __syncthreads();
-    for (int tile = t_begin; tile < t_end; tile += 2) {
-        tile_step(tile, s_k0, s_v0, s_absent0, s_k1, s_v1, s_absent1);
-        if (tile + 1 < t_end) tile_step(tile + 1, s_k1, s_v1, s_absent1, s_k0, s_v0, s_absent0);
+        load_v(t_begin, s_v0);
+        if (t_begin + 1 < t_end) load_k(t_begin + 1, s_k1, s_absent1);
+        look_up(t_begin + 2);
+        __builtin_amdgcn_s_waitcnt(0x0f70);
+        __syncthreads();
+        products(s_k0, s);
+        const LogitOf<CAP, BIAS> logit(a.mods, (float)(i_lane - t_begin * KT), slope2, 0.0f);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[e / 16][e % 16] = logit.any(s[e / 16][e % 16], key_row(e));
+        settle(t_begin, s, largest(s), s_absent0);
+        __syncthreads();
+        for (int tile = t_begin; tile < t_end; tile += 2) {
+            tile_step(tile, s, s_k1, s_v0, s_absent1, s_k0, s_v1, s_absent0);
+            if (tile + 1 < t_end) tile_step(tile + 1, s, s_k0, s_v1, s_absent0, s_k1, s_v0, s_absent1);
+        }
     }
 
     // ---- results
@@ -600,16 +687,14 @@ __global__ __launch_bounds__(64) void attend_few_kernel(RowsArgs a) {
 #pragma unroll
         for (int x = 0; x < NQ; ++x) {
             const float ref = top[x] == ninf ? 0.0f : top[x];
-            logits2<true>(a.mods, s[x], (float)(run.begin + ((16 * x + (lane & 15)) >> a.g_log2) - t0), slope2[x], ref,
-                    [&](int e) { return 16 * (e / 4) + 4 * g + e % 4; });
+            logits2(a.mods, s[x], (float)(run.begin + ((16 * x + (lane & 15)) >> a.g_log2) - 4 * g - t0), slope2[x], ref,
+                    [](int e) { return 16 * (e / 4) + e % 4; });
             if (__any(lo[x] > t0 || hi[x] < t0 + KT - 1) || gone) {
-                const uint32_t span = (uint32_t)(hi[x] - lo[x]);
-                const bool any = lo[x] <= hi[x];
+                const uint32_t span = lo[x] <= hi[x] ? (uint32_t)(hi[x] - lo[x]) : 0u;
+                const int from = lo[x] <= hi[x] ? t0 + 4 * g - lo[x] : -0x40000000;
 #pragma unroll
-                for (int e = 0; e < 4 * NT; ++e) {
-                    const bool vis = any && (uint32_t)(t0 + 16 * (e / 4) + 4 * g + e % 4 - lo[x]) <= span && !((gone >> (e / 4)) & 1);
-                    s[x][e] = vis ? s[x][e] : ninf;
-                }
+                for (int e = 0; e < 4 * NT; ++e)
+                    s[x][e] = (((uint32_t)(from + 16 * (e / 4) + e % 4) <= span) & !((gone >> (e / 4)) & 1)) ? s[x][e] : ninf;
             }
             float mx = s[x][0];
 #pragma unroll
@@ -795,18 +880,21 @@ __global__ __launch_bounds__(kRowsMergeThreads) void attend_rows_merge_kernel(Ro
     }
 }
 
-template <typename T, int D, bool GEN> static void launch_rows(const RowsArgs &a, dim3 grid, hipStream_t st) {
+template <typename T, int D, bool CAP, bool BIAS> static void launch_rows(const RowsArgs &a, dim3 grid, hipStream_t st) {
     if constexpr (sizeof(T) == 2) {
         if (a.out_dtype == SOCKET_F32) {
-            hipLaunchKernelGGL((attend_rows_kernel<T, D, 3, GEN>), grid, dim3(kRowsThreads), 0, st, a);
+            hipLaunchKernelGGL((attend_rows_kernel<T, D, 3, CAP, BIAS>), grid, dim3(kRowsThreads), 0, st, a);
             return;
         }
     }
-    hipLaunchKernelGGL((attend_rows_kernel<T, D, 1, GEN>), grid, dim3(kRowsThreads), 0, st, a);
+    hipLaunchKernelGGL((attend_rows_kernel<T, D, 1, CAP, BIAS>), grid, dim3(kRowsThreads), 0, st, a);
 }
 template <typename T, int D> static void launch_rows(const RowsArgs &a, dim3 grid, hipStream_t st) {
-    if (a.mods.a > 0.0f || a.mods.slopes) launch_rows<T, D, true>(a, grid, st);
-    else launch_rows<T, D, false>(a, grid, st);
+    const bool cap = a.mods.a > 0.0f, bias = a.mods.slopes != nullptr;
+    if (cap && bias) launch_rows<T, D, true, true>(a, grid, st);
+    else if (cap) launch_rows<T, D, true, false>(a, grid, st);
+    else if (bias) launch_rows<T, D, false, true>(a, grid, st);
+    else launch_rows<T, D, false, false>(a, grid, st);
 }
 
 template <typename T, int D> static void launch_few(const RowsArgs &a, bool wide, dim3 grid, hipStream_t st) {

@@ -159,18 +159,19 @@ __global__ __launch_bounds__(kMassThreads, D <= 128 ? 2 : 1) void key_mass_kerne
                 float s[16];
 #pragma unroll
                 for (int r = 0; r < 16; ++r) s[r] = c[y][r];
-                logits2<true>(a.mods, s, (float)(meta.i[n] - v0), meta.slope[n], lse, [&](int r) { return tile_row(r, hf); });
+                logits2(a.mods, s, (float)(meta.i[n] - 4 * hf - v0), meta.slope[n], lse, [](int r) { return tile_row(r, 0); });
                 if (__all(lo <= v0 && hi >= v0 + 31) && there[y] == 0xffffffffu) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) acc[y][r] += exp2_fast(s[r]);
                 } else {
-                    const uint32_t span = (uint32_t)(hi - lo);
+                    // (a row that sees nothing: every difference is negative, and so above the span 0)
+                    const uint32_t span = lo <= hi ? (uint32_t)(hi - lo) : 0u, have = there[y] >> (4 * hf);
+                    const int from = lo <= hi ? v0 + 4 * hf - lo : -0x40000000;
 #pragma unroll
                     for (int r = 0; r < 16; ++r) {
-                        const int row = tile_row(r, hf);
-                        const bool vis = lo <= hi && (uint32_t)(v0 + row - lo) <= span && ((there[y] >> row) & 1u);
+                        const int row = tile_row(r, 0);
                         const float p = exp2_fast(s[r]);
-                        acc[y][r] += vis ? p : 0.0f;
+                        acc[y][r] += (((uint32_t)(from + row) <= span) & ((have >> row) & 1u)) ? p : 0.0f;
                     }
                 }
             }
@@ -327,12 +328,13 @@ __global__ __launch_bounds__(64) void key_mass_few_kernel(MassArgs a) {
             float s[4 * NT];
 #pragma unroll
             for (int e = 0; e < 4 * NT; ++e) s[e] = c[x][e / 4][e % 4];
-            logits2<true>(a.mods, s, (float)(run.begin + ((first_m + 16 * x + (lane & 15)) >> a.g_log2) - t0), slope2[x], lse[x],
-                    [&](int e) { return 16 * (e / 4) + 4 * g + e % 4; });
-            const uint32_t span = (uint32_t)(hi[x] - lo[x]);
+            logits2(a.mods, s, (float)(run.begin + ((first_m + 16 * x + (lane & 15)) >> a.g_log2) - 4 * g - t0), slope2[x], lse[x],
+                    [](int e) { return 16 * (e / 4) + e % 4; });
+            const uint32_t span = lo[x] <= hi[x] ? (uint32_t)(hi[x] - lo[x]) : 0u;
+            const int from = lo[x] <= hi[x] ? t0 + 4 * g - lo[x] : -0x40000000;
 #pragma unroll
             for (int e = 0; e < 4 * NT; ++e) {
-                const bool vis = lo[x] <= hi[x] && (uint32_t)(t0 + 16 * (e / 4) + 4 * g + e % 4 - lo[x]) <= span && !((gone >> (e / 4)) & 1);
+                const bool vis = ((uint32_t)(from + 16 * (e / 4) + e % 4) <= span) & !((gone >> (e / 4)) & 1);
                 const float p = exp2_fast(s[e]);
                 sum[e] += vis ? p : 0.0f;
             }
