@@ -127,6 +127,11 @@ template <bool CAP, bool BIAS> struct LogitOf {
         most = fmaxf(most, fabsf(y));
         return biased(fmaf(y * a, tanh_ratio(y * y), -ref), row);
     }
+    // of an argument y that is scaled already (capped; else the dot product itself)
+    __device__ __forceinline__ float scaled(float y, int row, bool small_) const {
+        if (!CAP) return biased(fmaf(y, c, -ref), row);
+        return biased(small_ ? fmaf(y * a, tanh_ratio(y * y), -ref) : fmaf(a, tanh_any(y), -ref), row);
+    }
     __device__ __forceinline__ float any(float x, int row) const {
         return biased(CAP ? fmaf(a, tanh_any(x * c), -ref) : fmaf(x, c, -ref), row);
     }

@@ -401,17 +401,25 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D 
     // values beside the next tile's logits; the tile after that is on its way.  In stages of a few matrix instructions,
     // whose operands are read from LDS two stages before (the compiler's own order reads each right before its
     // use, and every matrix instruction waits for LDS) and the vector work of the softmax shared out among them.
+    auto sees = [&](int tile) __attribute__((always_inline)) {
+        const int t0 = base + tile * KT;
+        return __any(valid && lo <= t0 + KT - 1 && hi >= t0);
+    };
+    bool seen = true;                                // whether the wavefront sees the tile at hand
     auto tile_step = [&](int tile, floatx16_t (&s)[NU], const char *k_next, const char *v_now, const int *absent_next, char *k_to, char *v_to, int *absent_to) __attribute__((always_inline)) {
         using Values = ValueStages<T, D, PX>;
         constexpr int AHEAD = 2, RING = AHEAD + 1;
         u32x4_t fk[RING][NU];
         typename Values::Part fv[RING];
         Values values;
-#pragma unroll
-        for (int ks = 0; ks < AHEAD; ++ks) read_k(k_next, ks, fk[ks]);
         if (tile + 1 < t_end) load_v(tile + 1, v_to);
         if (tile + 2 < t_end) load_k(tile + 2, k_to, absent_to);
         look_up(tile + 3);
+        const bool was_seen = seen;
+        seen = tile + 1 < t_end && sees(tile + 1);
+        if (was_seen || seen) {                      // (neither: the logits are -inf, and stay it)
+#pragma unroll
+        for (int ks = 0; ks < AHEAD; ++ks) read_k(k_next, ks, fk[ks]);
         floatx16_t c[NU];                            // (behind the last tile: products of what the buffer holds, not used)
 #pragma unroll
         for (int u = 0; u < NU; ++u) c[u] = 0.0f;
@@ -459,6 +467,7 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D 
         }
 #pragma unroll
         for (int u = 0; u < NU; ++u) s[u] = c[u];
+        }
         __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): this wavefront's part of what comes next is there
         __syncthreads();
     };
@@ -880,6 +889,49 @@ __global__ __launch_bounds__(kRowsMergeThreads) void attend_rows_merge_kernel(Ro
     }
 }
 
+// The same for few splits of many queries: a wavefront each (2011 rows of 8 heads in 4 splits: 34 us with a
+// workgroup each).
+constexpr int kFewSplits = 16;
+template <int D>
+__global__ __launch_bounds__(256) void attend_rows_merge_few_kernel(RowsArgs a, int n_items) {
+    constexpr int PER = D / 64;
+    const int lane = threadIdx.x & 63, item = __builtin_amdgcn_readfirstlane(blockIdx.x * 4 + (threadIdx.x >> 6));
+    if (item >= n_items) return;
+    const int row = item / a.Hq, b = row / a.max_rows, r = row - b * a.max_rows;
+    const float *part = a.partials + (int64_t)item * a.n_split * (D + 2);
+    const float ninf = -__builtin_inff();
+    const float2 ml = lane < a.n_split ? *(const float2 *)&part[lane * (D + 2)] : make_float2(ninf, 0.0f);
+    float x[kFewSplits][PER];
+#pragma unroll
+    for (int s = 0; s < kFewSplits; ++s)
+#pragma unroll
+        for (int k = 0; k < PER; ++k)
+            if (s < a.n_split) x[s][k] = part[s * (D + 2) + 2 + lane + 64 * k];
+    const RowRun run(a.row_begin, a.row_count, b, a.max_rows, a.map.max_n);
+    if (r >= run.count) return;                      // (what was read is not used)
+    const float top = wave_max(ml.x), use = top == ninf ? 0.0f : top, w = exp2_fast(ml.x - use);
+    const float sum = row_sum<64>(w * ml.y);
+    float acc[PER];
+#pragma unroll
+    for (int k = 0; k < PER; ++k) acc[k] = 0.0f;
+#pragma unroll
+    for (int s = 0; s < kFewSplits; ++s) {
+        if (s < a.n_split) {
+            const float ws = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(w), s));
+            // (a split without keys has written no values)
+#pragma unroll
+            for (int k = 0; k < PER; ++k) acc[k] = ws != 0.0f ? fmaf(ws, x[s][k], acc[k]) : acc[k];
+        }
+    }
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        const float y = sum == 0.0f ? 0.0f : acc[k] / sum;
+        if (a.out_dtype == SOCKET_F32) ((float *)a.out)[(int64_t)item * D + lane + 64 * k] = y;
+        else ((uint16_t *)a.out)[(int64_t)item * D + lane + 64 * k] = f32_to_bf16_rne(y);
+    }
+    if (a.lse && lane == 0) a.lse[item] = sum == 0.0f ? ninf : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
 template <typename T, int D, bool CAP, bool BIAS> static void launch_rows(const RowsArgs &a, dim3 grid, hipStream_t st) {
     if constexpr (sizeof(T) == 2) {
         if (a.out_dtype == SOCKET_F32) {
@@ -909,6 +961,11 @@ template <typename T, int D> static void launch_few(const RowsArgs &a, bool wide
     }
     if (wide) hipLaunchKernelGGL((attend_few_kernel<T, D, 2, 1>), grid, dim3(64), lds, st, a);
     else hipLaunchKernelGGL((attend_few_kernel<T, D, 1, 1>), grid, dim3(64), lds, st, a);
+}
+
+template <int D> static void launch_rows_merge(const RowsArgs &a, bool few, int items, dim3 grid, hipStream_t st) {
+    if (few) hipLaunchKernelGGL(attend_rows_merge_few_kernel<D>, grid, dim3(256), 0, st, a, items);
+    else hipLaunchKernelGGL(attend_rows_merge_kernel<D>, grid, dim3(kRowsMergeThreads), 0, st, a);
 }
 
 static int pick_splits(int64_t wanted, int64_t most, int64_t room) {
@@ -964,11 +1021,14 @@ int launch_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void
         }
     }
     if (a.n_split > 1) {
-        const dim3 mg(g.Hq, max_rows, batch);
+        // (items fit 32 bits: their partial results do in the scratch)
+        const int items = batch * max_rows * g.Hq;
+        const bool few = a.n_split <= kFewSplits && items > 1024;
+        const dim3 mg = few ? dim3((items + 3) / 4) : dim3(g.Hq, max_rows, batch);
         switch (g.d) {
-            case 64: hipLaunchKernelGGL(attend_rows_merge_kernel<64>, mg, dim3(kRowsMergeThreads), 0, st, a); break;
-            case 128: hipLaunchKernelGGL(attend_rows_merge_kernel<128>, mg, dim3(kRowsMergeThreads), 0, st, a); break;
-            default: hipLaunchKernelGGL(attend_rows_merge_kernel<256>, mg, dim3(kRowsMergeThreads), 0, st, a); break;
+            case 64: launch_rows_merge<64>(a, few, items, mg, st); break;
+            case 128: launch_rows_merge<128>(a, few, items, mg, st); break;
+            default: launch_rows_merge<256>(a, few, items, mg, st); break;
         }
     }
     return record_hip(ctx, hipGetLastError());

@@ -45,9 +45,11 @@ __device__ __forceinline__ float kept_mass(const MassArgs &a, const RowRun &run,
 //      rows, the last by few, and with segments no workgroup has more to do than another.
 constexpr int kMassThreads = 256;
 
-template <typename T, int D> struct MassTile {
+template <typename T, int D, bool CAP, bool BIAS> constexpr bool kMassWide = sizeof(T) == 2 && D <= 128 && !CAP && !BIAS;
+template <typename T, int D, bool CAP, bool BIAS> struct MassTile {
     static constexpr int ROWB = D * (int)sizeof(T), CPR = ROWB / 16;
-    static constexpr int KW = sizeof(T) == 2 && D <= 128 ? 64 : 32, NK = KW / 32;        // keys per wavefront
+    static constexpr int KW = kMassWide<T, D, CAP, BIAS> ? 64 : 32, NK = KW / 32;        // keys per wavefront
+    static constexpr int WAVES = ROWB > 512 ? 1 : KW == 64 || ROWB > 256 ? 2 : 3;        // per SIMD
     static constexpr int QT = ROWB <= 512 ? 64 : 32, NU = QT / 32;                       // queries per tile
     static constexpr int BYTES = QT * ROWB, LOADS = QT * CPR / kMassThreads;
     static __device__ __forceinline__ int turned(int row, int c) { return c ^ (row & (CPR < 16 ? CPR - 1 : 15)); }
@@ -57,9 +59,9 @@ struct MassMeta {             // what a tile's queries bring beside their channe
     float lse[64], slope[64];
 };
 
-template <typename T, int D>
-__global__ __launch_bounds__(kMassThreads, D <= 128 ? 2 : 1) void key_mass_kernel(MassArgs a) {
-    using Tile = MassTile<T, D>;
+template <typename T, int D, bool CAP, bool BIAS>
+__global__ __launch_bounds__(kMassThreads) __attribute__((amdgpu_waves_per_eu(MassTile<T, D, CAP, BIAS>::WAVES, MassTile<T, D, CAP, BIAS>::WAVES))) void key_mass_kernel(MassArgs a) {
+    using Tile = MassTile<T, D, CAP, BIAS>;
     constexpr int ROWB = Tile::ROWB, CPR = Tile::CPR, NKS = CPR / 2, QT = Tile::QT, NU = Tile::NU, LOADS = Tile::LOADS;
     constexpr int KW = Tile::KW, NK = Tile::NK, KEYS = 4 * KW;
     __shared__ __align__(16) char s_q0[Tile::BYTES], s_q1[Tile::BYTES];
@@ -94,20 +96,37 @@ __global__ __launch_bounds__(kMassThreads, D <= 128 ? 2 : 1) void key_mass_kerne
             if (krow >= 0) k[y][ks] = *(const u32x4_t *)((const char *)a.K + krow * ROWB + (2 * ks + hf) * 16);
         }
     }
+    bool all_there = true;
+#pragma unroll
+    for (int y = 0; y < NK; ++y) all_there = all_there && there[y] == 0xffffffffu;
 
+    // Tiles start at whole rows (m_lo and QT are multiples of G), so a lane's byte in a turn of loads is the
+    // same for every tile and turn, but for where it starts.
+    constexpr int RPL = kMassThreads / CPR;          // queries that all wavefronts' loads of one turn cover
+    constexpr bool ONE_TURN = RPL % 16 == 0;
+    const int w_row = wave * 64 / CPR, l_row = lane / CPR, l_piece = lane % CPR;
+    const int64_t row_bytes = (int64_t)a.Hq * ROWB;
+    const char *const q_head = (const char *)a.q + (int64_t)b * a.max_rows * row_bytes + (int64_t)h * a.G * ROWB;
+    auto byte_of = [&](int p, int row) __attribute__((always_inline)) {      // of query `row` of a tile, in turn p
+        return (uint32_t)((row >> a.g_log2) * (a.Hq * ROWB) + (row & (a.G - 1)) * ROWB + Tile::turned((p * RPL + w_row) % 16 + l_row, l_piece) * 16);
+    };
+    const uint32_t q_byte = byte_of(0, w_row + l_row);
     int n_lo = 0, n_hi = -1, n_i = 0;
     float n_lse = 0.0f, n_slope = 0.0f;
-    const char *const q_head = (const char *)a.q + ((int64_t)b * a.max_rows * a.Hq + h * a.G) * ROWB;
     auto load = [&](int tile, char *qn) __attribute__((always_inline)) {
+        const int m0 = m_lo + tile * QT;
+        const char *from = q_head + (m0 >> a.g_log2) * row_bytes;
+        if (ONE_TURN && m0 + QT <= m_hi) {
 #pragma unroll
-        for (int p = 0; p < LOADS; ++p) {
-            const int slot = p * kMassThreads + wave * 64, row = (slot + lane) / CPR;
-            const int m = min(m_lo + tile * QT + row, m_hi - 1);
-            const char *src = q_head + ((int64_t)(m >> a.g_log2) * a.Hq + (m & (a.G - 1))) * ROWB + Tile::turned(row, (slot + lane) % CPR) * 16;
-            lds_fill(src, qn + slot * 16);
+            for (int p = 0; p < LOADS; ++p) lds_fill(from + (p * RPL >> a.g_log2) * row_bytes + q_byte, qn + (p * kMassThreads + wave * 64) * 16);
+        } else {
+#pragma unroll
+            for (int p = 0; p < LOADS; ++p)          // (queries behind the last read it again)
+                lds_fill(from + byte_of(p, min(p * RPL + w_row + l_row, m_hi - 1 - m0)), qn + (p * kMassThreads + wave * 64) * 16);
         }
-        if (tid < QT) {
-            const int m = m_lo + tile * QT + tid;
+        // what the tile's queries bring beside their channels: the wavefronts in turn
+        const int n = lane, m = m0 + n;
+        if ((tile & 3) == wave && n < QT) {
             n_lo = 0;
             n_hi = -1;
             if (m < m_hi) {
@@ -120,69 +139,129 @@ __global__ __launch_bounds__(kMassThreads, D <= 128 ? 2 : 1) void key_mass_kerne
             }
         }
     };
-    auto store_meta = [&](MassMeta &meta) __attribute__((always_inline)) {
-        if (tid < QT) {
-            meta.lo[tid] = n_lo;
-            meta.hi[tid] = n_hi;
-            meta.i[tid] = n_i;
-            meta.lse[tid] = n_lse;
-            meta.slope[tid] = n_slope;
+    auto store_meta = [&](int tile, MassMeta &meta) __attribute__((always_inline)) {
+        if ((tile & 3) == wave && lane < QT) {
+            meta.lo[lane] = n_lo;
+            meta.hi[lane] = n_hi;
+            meta.i[lane] = n_i;
+            meta.lse[lane] = n_lse;
+            if (BIAS) meta.slope[lane] = n_slope;
         }
     };
 
-    float acc[NK][16];
+    floatx16_t acc[NK];
 #pragma unroll
-    for (int y = 0; y < NK; ++y)
+    for (int y = 0; y < NK; ++y) acc[y] = 0.0f;
+    constexpr int E = 16 * NK, AHEAD = 2, RING = AHEAD + 1;
+    // products of the 32 queries u of a tile, in stages: operands are read two stages ahead, and `beside` runs
+    // between the matrix instructions
+    auto products = [&](const char *qt, int u, floatx16_t (&c)[NK], auto beside) __attribute__((always_inline)) {
+        const int n = 32 * u + (lane & 31);
+        u32x4_t f[RING];
+        auto read = [&](int ks) __attribute__((always_inline)) { return *(const u32x4_t *)(qt + (n * CPR + Tile::turned(n, 2 * ks + hf)) * 16); };
 #pragma unroll
-        for (int r = 0; r < 16; ++r) acc[y][r] = 0.0f;
+        for (int ks = 0; ks < AHEAD; ++ks) f[ks] = read(ks);
+#pragma unroll
+        for (int y = 0; y < NK; ++y) c[y] = 0.0f;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) {
+            if (ks + AHEAD < NKS) f[(ks + AHEAD) % RING] = read(ks + AHEAD);
+#pragma unroll
+            for (int y = 0; y < NK; ++y) mma_piece<T>(c[y], k[y][ks], f[ks % RING]);
+            beside(ks);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // what the 32 queries u add to the keys' masses, element by element, all keys seen
+    struct Query { int lo, hi; float lse, dist, slope; };
+    auto query = [&](const MassMeta &meta, int u) __attribute__((always_inline)) {
+        const int n = 32 * u + (lane & 31);
+        return Query{meta.lo[n], meta.hi[n], meta.lse[n], BIAS ? (float)(meta.i[n] - 4 * hf - w0) : 0.0f, BIAS ? meta.slope[n] : 0.0f};
+    };
+    auto key_row = [](int e) __attribute__((always_inline)) { return 32 * (e / 16) + tile_row(e % 16, 0); };
+    // sums of weights of products c (which become the logits): `whole` where every query sees every key of the
+    // wavefront
+    auto add_all = [&](floatx16_t (&c)[NK], const Query &x, bool whole) __attribute__((always_inline)) {
+        const LogitOf<CAP, BIAS> logit(a.mods, x.dist, x.slope, x.lse);
+        bool small = true;
+        if (CAP) {                                   // (scaled first: a wavefront whose arguments all are small takes the ratio alone)
+            float most = 0.0f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                c[e / 16][e % 16] *= logit.c;
+                most = fmaxf(most, fabsf(c[e / 16][e % 16]));
+            }
+            small = __all(most <= kCapSmall);
+        }
+        if (whole && small) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+                acc[e / 16][e % 16] += exp2_fast(logit.scaled(c[e / 16][e % 16], key_row(e), true));
+                if (e % 8 == 7) __builtin_amdgcn_sched_barrier(0);
+            }
+            return;
+        }
+        // (four at a time: more of them under way at once do not fit the registers)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            c[e / 16][e % 16] = logit.scaled(c[e / 16][e % 16], key_row(e), false);
+            if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+        // (a row that sees nothing: every difference is negative, and so above the span 0)
+        const uint32_t span = x.lo <= x.hi ? (uint32_t)(x.hi - x.lo) : 0u;
+        int from = x.lo <= x.hi ? w0 + 4 * hf - x.lo : -0x40000000;
+        asm volatile("" : "+v"(from));               // (its sums belong here, not ahead of the branch)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+            const float p = exp2_fast(c[e / 16][e % 16]);
+            const bool vis = ((uint32_t)(from + key_row(e)) <= span) & ((there[e / 16] >> (4 * hf) >> tile_row(e % 16, 0)) & 1u);
+            acc[e / 16][e % 16] += vis ? p : 0.0f;
+            if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+    };
     auto tile_step = [&](int tile, const char *qt, const MassMeta &meta, char *qn, MassMeta &meta_n) __attribute__((always_inline)) {
         const bool more = tile + 1 < t_end;
         if (more) load(tile + 1, qn);
+        floatx16_t c[NK], d[NK];
+        Query x = query(meta, 0);
+        // (whether any query sees any of the wavefront's keys, and all see all)
+        auto any_of = [&](const Query &y) { return __any(y.lo <= w0 + KW - 1 && y.hi >= w0 && y.lo <= y.hi); };
+        auto all_of = [&](const Query &y) { return __all(y.lo <= w0 && y.hi >= w0 + KW - 1) && all_there; };
+        if constexpr (NU == 2) {
+            const Query z = query(meta, 1);
+            if (!CAP && all_of(x) && all_of(z)) {
+                // the first half's exponentials beside the second's products (capped, the vector work alone is more than
+                // both: the other wavefront's products run beside it)
+                products(qt, 0, c, [](int) {});
+                const LogitOf<CAP, BIAS> first(a.mods, x.dist, x.slope, x.lse), second(a.mods, z.dist, z.slope, z.lse);
+                products(qt, 1, d, [&](int ks) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < NU; ++u) {
-            const int n = 32 * u + (lane & 31);
-            const int lo = meta.lo[n], hi = meta.hi[n];
-            if (!__any(lo <= w0 + KW - 1 && hi >= w0 && lo <= hi)) continue;
-            floatx16_t c[NK];
+                    for (int e = E * ks / NKS; e < E * (ks + 1) / NKS; ++e) acc[e / 16][e % 16] += exp2_fast(first.any(c[e / 16][e % 16], key_row(e)));
+                });
 #pragma unroll
-            for (int y = 0; y < NK; ++y) c[y] = 0.0f;
-#pragma unroll
-            for (int ks = 0; ks < NKS; ++ks) {
-                const u32x4_t qf = *(const u32x4_t *)(qt + (n * CPR + Tile::turned(n, 2 * ks + hf)) * 16);
-#pragma unroll
-                for (int y = 0; y < NK; ++y) mma_piece<T>(c[y], k[y][ks], qf);
-            }
-            const float lse = meta.lse[n];
-#pragma unroll
-            for (int y = 0; y < NK; ++y) {
-                const int v0 = w0 + 32 * y;
-                float s[16];
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] = c[y][r];
-                logits2(a.mods, s, (float)(meta.i[n] - 4 * hf - v0), meta.slope[n], lse, [](int r) { return tile_row(r, 0); });
-                if (__all(lo <= v0 && hi >= v0 + 31) && there[y] == 0xffffffffu) {
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) acc[y][r] += exp2_fast(s[r]);
-                } else {
-                    // (a row that sees nothing: every difference is negative, and so above the span 0)
-                    const uint32_t span = lo <= hi ? (uint32_t)(hi - lo) : 0u, have = there[y] >> (4 * hf);
-                    const int from = lo <= hi ? v0 + 4 * hf - lo : -0x40000000;
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        const int row = tile_row(r, 0);
-                        const float p = exp2_fast(s[r]);
-                        acc[y][r] += (((uint32_t)(from + row) <= span) & ((have >> row) & 1u)) ? p : 0.0f;
-                    }
+                for (int e = 0; e < E; ++e) acc[e / 16][e % 16] += exp2_fast(second.any(d[e / 16][e % 16], key_row(e)));
+            } else {
+                if (any_of(x)) {
+                    products(qt, 0, c, [](int) {});
+                    add_all(c, x, all_of(x));
+                }
+                if (any_of(z)) {
+                    products(qt, 1, c, [](int) {});
+                    add_all(c, z, all_of(z));
                 }
             }
+        } else if (any_of(x)) {
+            products(qt, 0, c, [](int) {});
+            add_all(c, x, all_of(x));
         }
-        if (more) store_meta(meta_n);
+        if (more) store_meta(tile + 1, meta_n);
         __builtin_amdgcn_s_waitcnt(0x0f70);          // vmcnt(0): this wavefront's part of the next tile is there
         __syncthreads();
     };
     if (t_begin < t_end) {
         load(t_begin, s_q0);
-        store_meta(s_meta0);
+        store_meta(t_begin, s_meta0);
     }
     __builtin_amdgcn_s_waitcnt(0x0f70);
     __syncthreads();
@@ -350,8 +429,23 @@ __global__ __launch_bounds__(64) void key_mass_few_kernel(MassArgs a) {
     }
 }
 
+template <typename T, int D, bool CAP, bool BIAS> static int launch_mass_tiles(MassArgs a, int64_t room, int max_n, int rows, hipStream_t st) {
+    using Tile = MassTile<T, D, CAP, BIAS>;
+    constexpr int KEYS = 4 * Tile::KW;
+    const int64_t tiles = ((int64_t)rows * a.G + Tile::QT - 1) / Tile::QT;
+    int64_t seg = (tiles + 31) / 32;
+    const int64_t fits = room / ((int64_t)a.BH * max_n);
+    seg = seg < fits ? seg : fits;
+    a.n_seg = seg < 1 ? 1 : (int)seg;
+    a.seg_tiles = (int)((tiles + a.n_seg - 1) / a.n_seg);
+    const int64_t grid = (int64_t)a.BH * ((max_n + KEYS - 1) / KEYS) * a.n_seg;
+    if (grid >= (int64_t)1 << 31) return SOCKET_EUNSUPPORTED;
+    hipLaunchKernelGGL((key_mass_kernel<T, D, CAP, BIAS>), dim3((unsigned)grid), dim3(kMassThreads), 0, st, a);
+    if (a.n_seg > 1) hipLaunchKernelGGL((key_mass_merge_kernel<KEYS, Tile::QT>), dim3((unsigned)((max_n + 255) / 256) * (unsigned)a.BH), dim3(256), 0, st, a);
+    return SOCKET_OK;
+}
+
 template <typename T, int D> static int launch_mass(MassArgs a, int64_t room, int max_n, int max_rows, hipStream_t st) {
-    using Tile = MassTile<T, D>;
     const int rows = a.last_rows > 0 && a.last_rows < max_rows ? a.last_rows : max_rows;
     if ((int64_t)rows * a.G <= 32) {
         // as many wavefronts as keep the card busy, 64 keys each at least
@@ -364,18 +458,9 @@ template <typename T, int D> static int launch_mass(MassArgs a, int64_t room, in
         else hipLaunchKernelGGL((key_mass_few_kernel<T, D, 1>), dim3((unsigned)grid), dim3(64), 0, st, a);
         return SOCKET_OK;
     }
-    constexpr int KEYS = 4 * Tile::KW;
-    const int64_t tiles = ((int64_t)rows * a.G + Tile::QT - 1) / Tile::QT;
-    int64_t seg = (tiles + 31) / 32;
-    const int64_t fits = room / ((int64_t)a.BH * max_n);
-    seg = seg < fits ? seg : fits;
-    a.n_seg = seg < 1 ? 1 : (int)seg;
-    a.seg_tiles = (int)((tiles + a.n_seg - 1) / a.n_seg);
-    const int64_t grid = (int64_t)a.BH * ((max_n + KEYS - 1) / KEYS) * a.n_seg;
-    if (grid >= (int64_t)1 << 31) return SOCKET_EUNSUPPORTED;
-    hipLaunchKernelGGL((key_mass_kernel<T, D>), dim3((unsigned)grid), dim3(kMassThreads), 0, st, a);
-    if (a.n_seg > 1) hipLaunchKernelGGL((key_mass_merge_kernel<KEYS, Tile::QT>), dim3((unsigned)((max_n + 255) / 256) * (unsigned)a.BH), dim3(256), 0, st, a);
-    return SOCKET_OK;
+    const bool cap = a.mods.a > 0.0f, bias = a.mods.slopes != nullptr;
+    return cap && bias ? launch_mass_tiles<T, D, true, true>(a, room, max_n, rows, st) : cap ? launch_mass_tiles<T, D, true, false>(a, room, max_n, rows, st)
+           : bias ? launch_mass_tiles<T, D, false, true>(a, room, max_n, rows, st) : launch_mass_tiles<T, D, false, false>(a, room, max_n, rows, st);
 }
 
 int launch_key_mass(socket_ctx *ctx, const void *q, const void *K, const float *lse, const int32_t *block_table,
