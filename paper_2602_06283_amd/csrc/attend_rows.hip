@@ -399,7 +399,7 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D 
     };
     // One tile, whose logits are there.  The exponentials run beside the products of the next tile's keys, its
     // values beside the next tile's logits; the tile after that is on its way.  In stages of a few matrix instructions,
-    // whose operands are read from LDS two stages before (the compiler's own order reads each right before its
+    // whose operands are read from LDS a stage before (the compiler's own order reads each right before its
     // use, and every matrix instruction waits for LDS) and the vector work of the softmax shared out among them.
     auto sees = [&](int tile) __attribute__((always_inline)) {
         const int t0 = base + tile * KT;
@@ -408,7 +408,7 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D 
     bool seen = true;                                // whether the wavefront sees the tile at hand
     auto tile_step = [&](int tile, floatx16_t (&s)[NU], const char *k_next, const char *v_now, const int *absent_next, char *k_to, char *v_to, int *absent_to) __attribute__((always_inline)) {
         using Values = ValueStages<T, D, PX>;
-        constexpr int AHEAD = 2, RING = AHEAD + 1;
+        constexpr int AHEAD = 1, RING = AHEAD + 1;
         u32x4_t fk[RING][NU];
         typename Values::Part fv[RING];
         Values values;
