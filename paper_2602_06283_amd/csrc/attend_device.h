@@ -218,7 +218,7 @@ __device__ __forceinline__ float sixteenths_max(float v) {
 
 // sizes and swizzles of the K / V tiles in LDS, in pieces of 16 bytes
 template <typename T, int D> struct KvTile {
-    static constexpr int KT = sizeof(T) == 2 ? 64 : 32;          // keys
+    static constexpr int KT = sizeof(T) == 2 && D <= 128 ? 64 : 32;          // keys
     static constexpr int ROWB = D * (int)sizeof(T);
     static constexpr int CPR = ROWB / 16;                        // pieces per row
     static constexpr int BYTES = KT * ROWB;

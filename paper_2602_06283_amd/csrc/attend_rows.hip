@@ -205,7 +205,8 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D 
     constexpr int LOADS = KT * CPR / kRowsThreads;               // pieces of K (and of V) a thread brings
     constexpr int NKS = CPR / 2;                                 // pairs of pieces along the channels
     __shared__ __align__(16) char s_k0[Tile::BYTES], s_v0[Tile::BYTES], s_k1[Tile::BYTES], s_v1[Tile::BYTES];
-    __shared__ __align__(16) int s_absent0[4], s_absent1[4];     // sixteenths of a tile whose block is absent
+    constexpr int kAhead = 64;                                   // tiles that are looked up together
+    __shared__ int s_rows[kAhead * NG];
     __shared__ int s_lo[4], s_hi[4];
 
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), hf = lane >> 5;
@@ -265,9 +266,9 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D 
     const int t_begin = split * per, t_end = min(n_tiles, t_begin + per);
 
     // ---- staging, straight from memory into LDS: a load of a wavefront fills 64 pieces in a row there, so the
-    //      turn of the pieces is done in the address it reads.  Its rows lie in one sixteenth of the cache
-    //      (a block holds whole ones): one scalar look-up, made a tile ahead.  A buffer is an array of its own, and the
-    //      loop goes over both: the compiler then sees that reads of one need not wait for the other's loads.
+    //      turn of the pieces is done in the address it reads.  Its rows lie in one sixteen of the cache (a block
+    //      holds whole ones).  A buffer is an array of its own, and the loop goes over both: the compiler then sees
+    //      that reads of one need not wait for the other's loads.
     constexpr int RPL = kRowsThreads / CPR;          // rows that all wavefronts' loads of one turn cover
     const bool paged = a.map.block_table != nullptr;
     const int w_row = wave * 64 / CPR, l_row = lane / CPR, l_piece = lane % CPR;      // first row of the wavefront in a turn, row and piece of the lane
@@ -278,22 +279,19 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D 
         return (uint32_t)(l_row * Tile::ROWB + (values ? Tile::v_turned(row, l_piece) : Tile::k_turned(row, l_piece)) * 16);
     };
     const uint32_t k_byte = byte_of(0, false), v_byte = byte_of(0, true);
-    const char *const k_head = (const char *)a.K + (paged ? (int64_t)h * a.map.page : (int64_t)bh * a.map.max_n + base) * Tile::ROWB;
-    const char *const v_head = (const char *)a.V + (paged ? (int64_t)h * a.map.page : (int64_t)bh * a.map.max_n + base) * Tile::ROWB;
-    const uint32_t block_bytes = (uint32_t)(a.map.Hkv * a.map.page * Tile::ROWB);
-    int blk_k[LOADS], blk_v[LOADS];
-#pragma unroll
-    for (int p = 0; p < LOADS; ++p) blk_k[p] = blk_v[p] = 0;
+    const int64_t head_row = paged ? 0 : (int64_t)bh * a.map.max_n + base;
+    const char *const k_head = (const char *)a.K + head_row * Tile::ROWB, *const v_head = (const char *)a.V + head_row * Tile::ROWB;
+    int looked_up = t_begin;
+    // Paged: the first rows of the sixteens of kAhead tiles, looked up together, wait in LDS (one by one, as
+    // scalar loads between the reads of the tiles, they held those up: 777 + 333 rows behind 5003 and 2001 107 us).
     auto look_up = [&](int tile) __attribute__((always_inline)) {
-        if (!paged) return;
-#pragma unroll
-        for (int p = 0; p < LOADS; ++p) {
-            blk_v[p] = blk_k[p];
-            if (tile >= t_end) continue;
-            blk_k[p] = scalar_load(&a.map.block_table[(int64_t)b * a.map.max_blocks + a.map.page_slot(min(base + tile * KT + p * RPL + w_row, k_hi))]);
+        looked_up = tile;
+        for (int x = tid; x < kAhead * NG; x += kRowsThreads) {
+            const int t = min(base + tile * KT + 16 * x, k_hi & ~15);
+            s_rows[x] = (int)a.map.row(b, h, t);     // (rows are numbered in 31 bits; -1: no block)
         }
     };
-    auto load_rows = [&](int tile, const char *head, uint32_t byte, char *to, const int (&blk)[LOADS], auto is_v) __attribute__((always_inline)) {
+    auto load_rows = [&](int tile, const char *head, uint32_t byte, char *to, auto is_v) __attribute__((always_inline)) {
         constexpr bool VALUES = decltype(is_v)::value;
         const int t0 = base + tile * KT;
         // (one branch per tile for the form of the address: address arithmetic was a third of the instructions)
@@ -303,27 +301,25 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D 
             for (int p = 0; p < LOADS; ++p)
                 lds_fill(from + p * RPL * Tile::ROWB + (ONE_TURN ? byte : byte_of(p, VALUES)), to + (p * kRowsThreads + wave * 64) * 16);
         } else {
+            int row[LOADS];
+            if (paged) {
+#pragma unroll
+                for (int p = 0; p < LOADS; ++p) row[p] = s_rows[(tile - looked_up) * NG + (p * RPL + w_row) / 16];
+            }
 #pragma unroll
             for (int p = 0; p < LOADS; ++p) {
-                // rows behind the last key read it again, sixteens behind it its own
-                const int first = min(t0 + p * RPL + w_row, k_hi);
-                const uint32_t in = (uint32_t)min(l_row, k_hi - first) * Tile::ROWB + (ONE_TURN ? byte : byte_of(p, VALUES)) - l_row * Tile::ROWB;
-                const bool gone = (unsigned)blk[p] >= (unsigned)(paged ? a.map.num_blocks : 1);
-                const char *from = head + (paged ? (uint64_t)(uint32_t)(gone ? 0 : blk[p]) * block_bytes + (int64_t)a.map.page_off(first) * Tile::ROWB
-                                                 : (uint64_t)(first - base) * Tile::ROWB);
-                lds_fill(from + in, to + (p * kRowsThreads + wave * 64) * 16);
+                const int in16 = (p * RPL + w_row) % 16;          // the wavefront's first row in its sixteen
+                const int first = min(t0 + p * RPL + w_row - in16, k_hi & ~15);
+                const int start = paged ? max(__builtin_amdgcn_readfirstlane(row[p]), 0) : first - base;
+                const char *from = head + (int64_t)start * Tile::ROWB;
+                // (rows behind the last key read it again)
+                const int in = min(in16 + l_row, k_hi - first);
+                lds_fill(from + (uint32_t)((in - l_row) * Tile::ROWB + (int)(ONE_TURN ? byte : byte_of(p, VALUES))), to + (p * kRowsThreads + wave * 64) * 16);
             }
         }
     };
-    auto load_k = [&](int tile, char *to, int *absent) __attribute__((always_inline)) {
-        if (paged) {
-#pragma unroll
-            for (int p = 0; p < LOADS; ++p)
-                if ((p * RPL + w_row) % 16 == 0 && lane == 0) absent[(p * RPL + w_row) / 16] = (unsigned)blk_k[p] >= (unsigned)a.map.num_blocks;
-        }
-        load_rows(tile, k_head, k_byte, to, blk_k, BoolTag<false>());
-    };
-    auto load_v = [&](int tile, char *to) __attribute__((always_inline)) { load_rows(tile, v_head, v_byte, to, blk_v, BoolTag<true>()); };
+    auto load_k = [&](int tile, char *to) __attribute__((always_inline)) { load_rows(tile, k_head, k_byte, to, BoolTag<false>()); };
+    auto load_v = [&](int tile, char *to) __attribute__((always_inline)) { load_rows(tile, v_head, v_byte, to, BoolTag<true>()); };
 
     floatx16_t o[D / 32];
 #pragma unroll
@@ -364,12 +360,12 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D 
         return across(mx);
     };
     // masks, and `top` raised where a logit asks for it
-    auto settle = [&](int tile, floatx16_t (&s)[NU], float mx, const int *absent) __attribute__((always_inline)) {
+    auto settle = [&](int tile, floatx16_t (&s)[NU], float mx) __attribute__((always_inline)) {
         const int t0 = base + tile * KT;
         int gone = 0;
-        if (a.map.block_table) {
+        if (paged) {
 #pragma unroll
-            for (int g = 0; g < NG; ++g) gone |= absent[g] << g;
+            for (int g = 0; g < NG; ++g) gone |= (s_rows[(tile - looked_up) * NG + g] < 0) << g;
             gone = __builtin_amdgcn_readfirstlane(gone);
         }
         if (__any(valid && (lo > t0 || hi < t0 + KT - 1)) || gone) {
@@ -406,15 +402,18 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D 
         return __any(valid && lo <= t0 + KT - 1 && hi >= t0);
     };
     bool seen = true;                                // whether the wavefront sees the tile at hand
-    auto tile_step = [&](int tile, floatx16_t (&s)[NU], const char *k_next, const char *v_now, const int *absent_next, char *k_to, char *v_to, int *absent_to) __attribute__((always_inline)) {
+    auto tile_step = [&](int tile, floatx16_t (&s)[NU], const char *k_next, const char *v_now, char *k_to, char *v_to) __attribute__((always_inline)) {
         using Values = ValueStages<T, D, PX>;
         constexpr int AHEAD = 1, RING = AHEAD + 1;
         u32x4_t fk[RING][NU];
         typename Values::Part fv[RING];
         Values values;
+        if (paged && tile + 3 - looked_up > kAhead) {
+            look_up(tile + 1);                       // (the barrier behind the last tile: its readers are done)
+            __syncthreads();
+        }
         if (tile + 1 < t_end) load_v(tile + 1, v_to);
-        if (tile + 2 < t_end) load_k(tile + 2, k_to, absent_to);
-        look_up(tile + 3);
+        if (tile + 2 < t_end) load_k(tile + 2, k_to);
         const bool was_seen = seen;
         seen = tile + 1 < t_end && sees(tile + 1);
         if (was_seen || seen) {                      // (neither: the logits are -inf, and stay it)
@@ -463,7 +462,7 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D 
                 for (int e = 0; e < E; ++e) c[e / 16][e % 16] = logit.any(c[e / 16][e % 16], key_row(e));
                 mx = largest(c);
             }
-            settle(tile + 1, c, mx, absent_next);
+            settle(tile + 1, c, mx);
         }
 #pragma unroll
         for (int u = 0; u < NU; ++u) s[u] = c[u];
@@ -473,23 +472,24 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D 
     };
     if (t_begin < t_end) {
         floatx16_t s[NU];
-        look_up(t_begin);
-        load_k(t_begin, s_k0, s_absent0);
-        look_up(t_begin + 1);
+        if (paged) {
+            look_up(t_begin);
+            __syncthreads();
+        }
+        load_k(t_begin, s_k0);
         load_v(t_begin, s_v0);
-        if (t_begin + 1 < t_end) load_k(t_begin + 1, s_k1, s_absent1);
-        look_up(t_begin + 2);
+        if (t_begin + 1 < t_end) load_k(t_begin + 1, s_k1);
         __builtin_amdgcn_s_waitcnt(0x0f70);
         __syncthreads();
         products(s_k0, s);
         const LogitOf<CAP, BIAS> logit(a.mods, (float)(i_lane - t_begin * KT), slope2, 0.0f);
 #pragma unroll
         for (int e = 0; e < E; ++e) s[e / 16][e % 16] = logit.any(s[e / 16][e % 16], key_row(e));
-        settle(t_begin, s, largest(s), s_absent0);
+        settle(t_begin, s, largest(s));
         __syncthreads();
         for (int tile = t_begin; tile < t_end; tile += 2) {
-            tile_step(tile, s, s_k1, s_v0, s_absent1, s_k0, s_v1, s_absent0);
-            if (tile + 1 < t_end) tile_step(tile + 1, s, s_k0, s_v1, s_absent0, s_k1, s_v0, s_absent1);
+            tile_step(tile, s, s_k1, s_v0, s_k0, s_v1);
+            if (tile + 1 < t_end) tile_step(tile + 1, s, s_k0, s_v1, s_k1, s_v0);
         }
     }
 
@@ -560,19 +560,20 @@ __global__ __launch_bounds__(64) void attend_few_kernel(RowsArgs a) {
     char *const kt = few_tiles, *const vt = few_tiles + Tile::BYTES;
 
     const int lane = threadIdx.x, g = lane >> 4;
-    const int bh = (int)blockIdx.x % a.BH, split = (int)blockIdx.x / a.BH;
+    const int bh = (int)blockIdx.x % a.BH, rest = (int)blockIdx.x / a.BH;
+    const int m0 = rest % a.n_tiles * 16 * NQ, split = rest / a.n_tiles;     // (column blocks side by side: they read the same keys)
     const int b = bh / a.map.Hkv, h = bh - b * a.map.Hkv;
     const RowRun run(a.row_begin, a.row_count, b, a.max_rows, a.map.max_n);
     const int n_m = run.count * a.G;
-    if (n_m == 0) return;
+    if (m0 >= n_m) return;
 
-    // ---- queries of column block x: m = 16 x + lane % 16
+    // ---- queries of column block x: m = m0 + 16 x + lane % 16
     int lo[NQ], hi[NQ], lo_w = 0x7fffffff, hi_w = -1;
     u32x4_t q[NQ][NKS];
     float slope2[NQ];
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
-        const int m = 16 * x + (lane & 15);
+        const int m = m0 + 16 * x + (lane & 15);
         lo[x] = 0x7fffffff;
         hi[x] = -1;
         slope2[x] = 0.0f;
@@ -696,7 +697,7 @@ __global__ __launch_bounds__(64) void attend_few_kernel(RowsArgs a) {
 #pragma unroll
         for (int x = 0; x < NQ; ++x) {
             const float ref = top[x] == ninf ? 0.0f : top[x];
-            logits2(a.mods, s[x], (float)(run.begin + ((16 * x + (lane & 15)) >> a.g_log2) - 4 * g - t0), slope2[x], ref,
+            logits2(a.mods, s[x], (float)(run.begin + ((m0 + 16 * x + (lane & 15)) >> a.g_log2) - 4 * g - t0), slope2[x], ref,
                     [](int e) { return 16 * (e / 4) + e % 4; });
             if (__any(lo[x] > t0 || hi[x] < t0 + KT - 1) || gone) {
                 const uint32_t span = lo[x] <= hi[x] ? (uint32_t)(hi[x] - lo[x]) : 0u;
@@ -770,7 +771,7 @@ __global__ __launch_bounds__(64) void attend_few_kernel(RowsArgs a) {
     // ---- results
 #pragma unroll
     for (int x = 0; x < NQ; ++x) {
-        const int m = 16 * x + (lane & 15);
+        const int m = m0 + 16 * x + (lane & 15);
         const float total = xor32_sum(xor16_sum(sum[x]));
         float check = 0.0f * total;
 #pragma unroll
@@ -806,7 +807,7 @@ __global__ __launch_bounds__(64) void attend_few_kernel(RowsArgs a) {
         while (again) {
             const int n = __builtin_ctzll(again);
             again &= again - 1;
-            const int mq = 16 * x + n;
+            const int mq = m0 + 16 * x + n;
             const int nlo = max(__builtin_amdgcn_readlane(lo[x], n), base + t_begin * KT);
             const int nhi = min(__builtin_amdgcn_readlane(hi[x], n), base + t_end * KT - 1);
             attend_plain<T, D>(a, b, h, mq, run.begin + (mq >> a.g_log2), nlo, nhi, split);
@@ -949,18 +950,22 @@ template <typename T, int D> static void launch_rows(const RowsArgs &a, dim3 gri
     else launch_rows<T, D, false, false>(a, grid, st);
 }
 
-template <typename T, int D> static void launch_few(const RowsArgs &a, bool wide, dim3 grid, hipStream_t st) {
+template <typename T, int D, int PX> static void launch_few(const RowsArgs &a, bool wide, dim3 grid, hipStream_t st) {
     constexpr size_t lds = 2 * FewTile<T, D>::BYTES;
     static_assert(lds <= 64 * 1024, "within the default dynamic LDS limit");
-    if constexpr (sizeof(T) == 2) {
-        if (a.out_dtype == SOCKET_F32) {
-            if (wide) hipLaunchKernelGGL((attend_few_kernel<T, D, 2, 3>), grid, dim3(64), lds, st, a);
-            else hipLaunchKernelGGL((attend_few_kernel<T, D, 1, 3>), grid, dim3(64), lds, st, a);
+    if constexpr (D < 256) {
+        if (wide) {
+            hipLaunchKernelGGL((attend_few_kernel<T, D, 2, PX>), grid, dim3(64), lds, st, a);
             return;
         }
     }
-    if (wide) hipLaunchKernelGGL((attend_few_kernel<T, D, 2, 1>), grid, dim3(64), lds, st, a);
-    else hipLaunchKernelGGL((attend_few_kernel<T, D, 1, 1>), grid, dim3(64), lds, st, a);
+    hipLaunchKernelGGL((attend_few_kernel<T, D, 1, PX>), grid, dim3(64), lds, st, a);
+}
+template <typename T, int D> static void launch_few(const RowsArgs &a, bool wide, dim3 grid, hipStream_t st) {
+    if constexpr (sizeof(T) == 2) {
+        if (a.out_dtype == SOCKET_F32) return launch_few<T, D, 3>(a, wide, grid, st);
+    }
+    launch_few<T, D, 1>(a, wide, grid, st);
 }
 
 template <int D> static void launch_rows_merge(const RowsArgs &a, bool few, int items, dim3 grid, hipStream_t st) {
@@ -992,12 +997,14 @@ int launch_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void
     if ((int64_t)max_rows * g.G <= 32) {
         // One wavefront a split, at least a tile of keys each: with 16 and more of them to a compute unit the last
         // ones to finish are a small part.
-        a.n_tiles = 1;
-        a.n_split = pick_splits(8192 / a.BH, (g.max_n + 31) / 32, room);
-        const int64_t grid = (int64_t)a.BH * a.n_split;
+        // More than 16 queries are two column blocks of a wavefront, at d = 256 (whose registers do not hold
+        // two: 8 rows of 4 heads behind 32000 151 us) of two wavefronts.
+        const bool two = max_rows * g.G > 16, wide = two && g.d < 256;
+        a.n_tiles = two && !wide ? 2 : 1;
+        a.n_split = pick_splits(8192 / (a.BH * a.n_tiles), (g.max_n + 31) / 32, room);
+        const int64_t grid = (int64_t)a.BH * a.n_tiles * a.n_split;
         if (grid >= (int64_t)1 << 31) return SOCKET_EUNSUPPORTED;
         const dim3 gr((unsigned)grid);
-        const bool wide = max_rows * g.G > 16;
         switch (g.d) {
             case 64: f32 ? launch_few<float, 64>(a, wide, gr, st) : launch_few<uint16_t, 64>(a, wide, gr, st); break;
             case 128: f32 ? launch_few<float, 128>(a, wide, gr, st) : launch_few<uint16_t, 128>(a, wide, gr, st); break;

@@ -39,17 +39,16 @@ __device__ __forceinline__ float kept_mass(const MassArgs &a, const RowRun &run,
     return j < run.begin && a.decay != 0.0f ? fmaf(a.decay, old, mine) : mine;
 }
 
-// ---- many queries: a workgroup's four wavefronts own KW keys each and share the queries, 64 at a
-//      time, in two LDS buffers that are filled straight from memory.  Long runs are cut into segments
-//      of seg_tiles tiles, whose sums a second launch adds up: the first keys of a prompt are seen by all of its
-//      rows, the last by few, and with segments no workgroup has more to do than another.
-constexpr int kMassThreads = 256;
+// ---- many queries: a workgroup's four wavefronts own 32 keys each and share the queries, 64 at a time, in
+//      two LDS buffers that are filled straight from memory.  (64 keys each read half as much of LDS, but their
+//      registers leave room for two wavefronts a SIMD, not three: 4096 rows 128 us against 118.)  Long runs are cut into
+//      segments of 16 tiles, whose sums a second launch adds up: the first keys of a prompt are seen by all of
+//      its rows, the last by few, and with segments no workgroup has more to do than another.
+constexpr int kMassThreads = 256, kMassKeys = 128;
 
-template <typename T, int D, bool CAP, bool BIAS> constexpr bool kMassWide = sizeof(T) == 2 && D <= 128 && !CAP && !BIAS;
-template <typename T, int D, bool CAP, bool BIAS> struct MassTile {
+template <typename T, int D> struct MassTile {
     static constexpr int ROWB = D * (int)sizeof(T), CPR = ROWB / 16;
-    static constexpr int KW = kMassWide<T, D, CAP, BIAS> ? 64 : 32, NK = KW / 32;        // keys per wavefront
-    static constexpr int WAVES = ROWB > 512 ? 1 : KW == 64 || ROWB > 256 ? 2 : 3;        // per SIMD
+    static constexpr int WAVES = ROWB > 512 ? 1 : ROWB > 256 ? 2 : 3;                    // per SIMD
     static constexpr int QT = ROWB <= 512 ? 64 : 32, NU = QT / 32;                       // queries per tile
     static constexpr int BYTES = QT * ROWB, LOADS = QT * CPR / kMassThreads;
     static __device__ __forceinline__ int turned(int row, int c) { return c ^ (row & (CPR < 16 ? CPR - 1 : 15)); }
@@ -60,10 +59,9 @@ struct MassMeta {             // what a tile's queries bring beside their channe
 };
 
 template <typename T, int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(kMassThreads) __attribute__((amdgpu_waves_per_eu(MassTile<T, D, CAP, BIAS>::WAVES, MassTile<T, D, CAP, BIAS>::WAVES))) void key_mass_kernel(MassArgs a) {
-    using Tile = MassTile<T, D, CAP, BIAS>;
+__global__ __launch_bounds__(kMassThreads) __attribute__((amdgpu_waves_per_eu(MassTile<T, D>::WAVES, MassTile<T, D>::WAVES))) void key_mass_kernel(MassArgs a) {
+    using Tile = MassTile<T, D>;
     constexpr int ROWB = Tile::ROWB, CPR = Tile::CPR, NKS = CPR / 2, QT = Tile::QT, NU = Tile::NU, LOADS = Tile::LOADS;
-    constexpr int KW = Tile::KW, NK = Tile::NK, KEYS = 4 * KW;
     __shared__ __align__(16) char s_q0[Tile::BYTES], s_q1[Tile::BYTES];
     __shared__ MassMeta s_meta0, s_meta1;
 
@@ -72,9 +70,9 @@ __global__ __launch_bounds__(kMassThreads) __attribute__((amdgpu_waves_per_eu(Ma
     const int seg = rest % a.n_seg, kb = rest / a.n_seg;
     const int b = bh / a.map.Hkv, h = bh - b * a.map.Hkv;
     const RowRun run(a.row_begin, a.row_count, b, a.max_rows, a.map.max_n);
-    const int j0 = kb * KEYS, len = run.len();
+    const int j0 = kb * kMassKeys, len = run.len();
     if (run.count == 0 || j0 >= len) return;
-    const int j1 = min(j0 + KEYS, len) - 1;
+    const int j1 = min(j0 + kMassKeys, len) - 1;
     int m_lo, m_hi;
     queries_of(a, run, b, j0, j1, m_lo, m_hi);
     // segment 0 is there for every key, also one that no query sees (its mass still decays)
@@ -82,23 +80,15 @@ __global__ __launch_bounds__(kMassThreads) __attribute__((amdgpu_waves_per_eu(Ma
     if (seg > 0 && t_begin >= t_all) return;
 
     // ---- this wavefront's keys, in registers
-    const int w0 = j0 + wave * KW;
-    uint32_t there[NK];
-    u32x4_t k[NK][NKS];
+    const int w0 = j0 + wave * 32, kj = w0 + (lane & 31);
+    const int64_t krow = kj <= j1 ? a.map.row(b, h, kj) : -1;
+    const uint32_t there = (uint32_t)__ballot(krow >= 0);
+    u32x4_t k[NKS];
 #pragma unroll
-    for (int y = 0; y < NK; ++y) {
-        const int kj = w0 + 32 * y + (lane & 31);
-        const int64_t krow = kj <= j1 ? a.map.row(b, h, kj) : -1;
-        there[y] = (uint32_t)__ballot(krow >= 0);
-#pragma unroll
-        for (int ks = 0; ks < NKS; ++ks) {
-            k[y][ks] = 0;
-            if (krow >= 0) k[y][ks] = *(const u32x4_t *)((const char *)a.K + krow * ROWB + (2 * ks + hf) * 16);
-        }
+    for (int ks = 0; ks < NKS; ++ks) {
+        k[ks] = 0;
+        if (krow >= 0) k[ks] = *(const u32x4_t *)((const char *)a.K + krow * ROWB + (2 * ks + hf) * 16);
     }
-    bool all_there = true;
-#pragma unroll
-    for (int y = 0; y < NK; ++y) all_there = all_there && there[y] == 0xffffffffu;
 
     // Tiles start at whole rows (m_lo and QT are multiples of G), so a lane's byte in a turn of loads is the
     // same for every tile and turn, but for where it starts.
@@ -149,26 +139,22 @@ __global__ __launch_bounds__(kMassThreads) __attribute__((amdgpu_waves_per_eu(Ma
         }
     };
 
-    floatx16_t acc[NK];
-#pragma unroll
-    for (int y = 0; y < NK; ++y) acc[y] = 0.0f;
-    constexpr int E = 16 * NK, AHEAD = 2, RING = AHEAD + 1;
+    floatx16_t acc = 0.0f;
+    constexpr int AHEAD = 2, RING = AHEAD + 1;
     // products of the 32 queries u of a tile, in stages: operands are read two stages ahead, and `beside` runs
     // between the matrix instructions
-    auto products = [&](const char *qt, int u, floatx16_t (&c)[NK], auto beside) __attribute__((always_inline)) {
+    auto products = [&](const char *qt, int u, floatx16_t &c, auto beside) __attribute__((always_inline)) {
         const int n = 32 * u + (lane & 31);
         u32x4_t f[RING];
         auto read = [&](int ks) __attribute__((always_inline)) { return *(const u32x4_t *)(qt + (n * CPR + Tile::turned(n, 2 * ks + hf)) * 16); };
 #pragma unroll
         for (int ks = 0; ks < AHEAD; ++ks) f[ks] = read(ks);
-#pragma unroll
-        for (int y = 0; y < NK; ++y) c[y] = 0.0f;
+        c = 0.0f;
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks) {
             if (ks + AHEAD < NKS) f[(ks + AHEAD) % RING] = read(ks + AHEAD);
-#pragma unroll
-            for (int y = 0; y < NK; ++y) mma_piece<T>(c[y], k[y][ks], f[ks % RING]);
+            mma_piece<T>(c, k[ks], f[ks % RING]);
             beside(ks);
             __builtin_amdgcn_sched_barrier(0);
         }
@@ -179,33 +165,33 @@ __global__ __launch_bounds__(kMassThreads) __attribute__((amdgpu_waves_per_eu(Ma
         const int n = 32 * u + (lane & 31);
         return Query{meta.lo[n], meta.hi[n], meta.lse[n], BIAS ? (float)(meta.i[n] - 4 * hf - w0) : 0.0f, BIAS ? meta.slope[n] : 0.0f};
     };
-    auto key_row = [](int e) __attribute__((always_inline)) { return 32 * (e / 16) + tile_row(e % 16, 0); };
+    auto key_row = [](int e) __attribute__((always_inline)) { return tile_row(e, 0); };
     // sums of weights of products c (which become the logits): `whole` where every query sees every key of the
     // wavefront
-    auto add_all = [&](floatx16_t (&c)[NK], const Query &x, bool whole) __attribute__((always_inline)) {
+    auto add_all = [&](floatx16_t &c, const Query &x, bool whole) __attribute__((always_inline)) {
         const LogitOf<CAP, BIAS> logit(a.mods, x.dist, x.slope, x.lse);
         bool small = true;
         if (CAP) {                                   // (scaled first: a wavefront whose arguments all are small takes the ratio alone)
             float most = 0.0f;
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                c[e / 16][e % 16] *= logit.c;
-                most = fmaxf(most, fabsf(c[e / 16][e % 16]));
+            for (int e = 0; e < 16; ++e) {
+                c[e] *= logit.c;
+                most = fmaxf(most, fabsf(c[e]));
             }
             small = __all(most <= kCapSmall);
         }
         if (whole && small) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                acc[e / 16][e % 16] += exp2_fast(logit.scaled(c[e / 16][e % 16], key_row(e), true));
+            for (int e = 0; e < 16; ++e) {
+                acc[e] += exp2_fast(logit.scaled(c[e], key_row(e), true));
                 if (e % 8 == 7) __builtin_amdgcn_sched_barrier(0);
             }
             return;
         }
         // (four at a time: more of them under way at once do not fit the registers)
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            c[e / 16][e % 16] = logit.scaled(c[e / 16][e % 16], key_row(e), false);
+        for (int e = 0; e < 16; ++e) {
+            c[e] = logit.scaled(c[e], key_row(e), false);
             if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
         // (a row that sees nothing: every difference is negative, and so above the span 0)
@@ -213,21 +199,21 @@ __global__ __launch_bounds__(kMassThreads) __attribute__((amdgpu_waves_per_eu(Ma
         int from = x.lo <= x.hi ? w0 + 4 * hf - x.lo : -0x40000000;
         asm volatile("" : "+v"(from));               // (its sums belong here, not ahead of the branch)
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            const float p = exp2_fast(c[e / 16][e % 16]);
-            const bool vis = ((uint32_t)(from + key_row(e)) <= span) & ((there[e / 16] >> (4 * hf) >> tile_row(e % 16, 0)) & 1u);
-            acc[e / 16][e % 16] += vis ? p : 0.0f;
+        for (int e = 0; e < 16; ++e) {
+            const float p = exp2_fast(c[e]);
+            const bool vis = ((uint32_t)(from + key_row(e)) <= span) & ((there >> (4 * hf) >> tile_row(e, 0)) & 1u);
+            acc[e] += vis ? p : 0.0f;
             if (e % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
     };
     auto tile_step = [&](int tile, const char *qt, const MassMeta &meta, char *qn, MassMeta &meta_n) __attribute__((always_inline)) {
         const bool more = tile + 1 < t_end;
         if (more) load(tile + 1, qn);
-        floatx16_t c[NK], d[NK];
+        floatx16_t c, d;
         Query x = query(meta, 0);
         // (whether any query sees any of the wavefront's keys, and all see all)
-        auto any_of = [&](const Query &y) { return __any(y.lo <= w0 + KW - 1 && y.hi >= w0 && y.lo <= y.hi); };
-        auto all_of = [&](const Query &y) { return __all(y.lo <= w0 && y.hi >= w0 + KW - 1) && all_there; };
+        auto any_of = [&](const Query &y) { return __any(y.lo <= w0 + 31 && y.hi >= w0 && y.lo <= y.hi); };
+        auto all_of = [&](const Query &y) { return __all(y.lo <= w0 && y.hi >= w0 + 31) && there == 0xffffffffu; };
         if constexpr (NU == 2) {
             const Query z = query(meta, 1);
             if (!CAP && all_of(x) && all_of(z)) {
@@ -237,10 +223,10 @@ __global__ __launch_bounds__(kMassThreads) __attribute__((amdgpu_waves_per_eu(Ma
                 const LogitOf<CAP, BIAS> first(a.mods, x.dist, x.slope, x.lse), second(a.mods, z.dist, z.slope, z.lse);
                 products(qt, 1, d, [&](int ks) __attribute__((always_inline)) {
 #pragma unroll
-                    for (int e = E * ks / NKS; e < E * (ks + 1) / NKS; ++e) acc[e / 16][e % 16] += exp2_fast(first.any(c[e / 16][e % 16], key_row(e)));
+                    for (int e = 16 * ks / NKS; e < 16 * (ks + 1) / NKS; ++e) acc[e] += exp2_fast(first.any(c[e], key_row(e)));
                 });
 #pragma unroll
-                for (int e = 0; e < E; ++e) acc[e / 16][e % 16] += exp2_fast(second.any(d[e / 16][e % 16], key_row(e)));
+                for (int e = 0; e < 16; ++e) acc[e] += exp2_fast(second.any(d[e], key_row(e)));
             } else {
                 if (any_of(x)) {
                     products(qt, 0, c, [](int) {});
@@ -273,31 +259,28 @@ __global__ __launch_bounds__(kMassThreads) __attribute__((amdgpu_waves_per_eu(Ma
     // ---- over the 32 queries of a tile, then lane r of either half writes register r's key
     float *const part = a.partials + ((int64_t)bh * a.n_seg + seg) * a.map.max_n;
     float *const mass = a.mass + (int64_t)bh * a.map.max_n;
+    float mine = 0.0f;
 #pragma unroll
-    for (int y = 0; y < NK; ++y) {
-        float mine = 0.0f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            const float t = row_sum<32>(acc[y][r]);
-            mine = (lane & 31) == r ? t : mine;
-        }
-        const int r = lane & 15, j = w0 + 32 * y + 8 * (r / 4) + 4 * hf + r % 4;
-        if ((lane & 31) < 16 && j <= j1) {
-            if (a.n_seg > 1) part[j] = mine;
-            else mass[j] = kept_mass(a, run, j, mass[j], mine);
-        }
+    for (int r = 0; r < 16; ++r) {
+        const float t = row_sum<32>(acc[r]);
+        mine = (lane & 31) == r ? t : mine;
+    }
+    const int r = lane & 15, j = w0 + 8 * (r / 4) + 4 * hf + r % 4;
+    if ((lane & 31) < 16 && j <= j1) {
+        if (a.n_seg > 1) part[j] = mine;
+        else mass[j] = kept_mass(a, run, j, mass[j], mine);
     }
 }
 
 // adds up the segments, in order
-template <int KEYS, int QT>
+template <int QT>
 __global__ __launch_bounds__(256) void key_mass_merge_kernel(MassArgs a) {
     const int bh = (int)blockIdx.x % a.BH, j = (int)blockIdx.x / a.BH * 256 + threadIdx.x, b = bh / a.map.Hkv;
     const RowRun run(a.row_begin, a.row_count, b, a.max_rows, a.map.max_n);
     if (run.count == 0 || j >= run.len()) return;
-    const int j0 = j / KEYS * KEYS;
+    const int j0 = j / kMassKeys * kMassKeys;
     int m_lo, m_hi;
-    queries_of(a, run, b, j0, min(j0 + KEYS, run.len()) - 1, m_lo, m_hi);
+    queries_of(a, run, b, j0, min(j0 + kMassKeys, run.len()) - 1, m_lo, m_hi);
     const int tiles = (m_hi - m_lo + QT - 1) / QT, n = max(1, (tiles + a.seg_tiles - 1) / a.seg_tiles);
     const float *part = a.partials + (int64_t)bh * a.n_seg * a.map.max_n + j;
     float sum = 0.0f;
@@ -430,18 +413,17 @@ __global__ __launch_bounds__(64) void key_mass_few_kernel(MassArgs a) {
 }
 
 template <typename T, int D, bool CAP, bool BIAS> static int launch_mass_tiles(MassArgs a, int64_t room, int max_n, int rows, hipStream_t st) {
-    using Tile = MassTile<T, D, CAP, BIAS>;
-    constexpr int KEYS = 4 * Tile::KW;
+    using Tile = MassTile<T, D>;
     const int64_t tiles = ((int64_t)rows * a.G + Tile::QT - 1) / Tile::QT;
-    int64_t seg = (tiles + 31) / 32;
+    int64_t seg = (tiles + 15) / 16;
     const int64_t fits = room / ((int64_t)a.BH * max_n);
     seg = seg < fits ? seg : fits;
     a.n_seg = seg < 1 ? 1 : (int)seg;
     a.seg_tiles = (int)((tiles + a.n_seg - 1) / a.n_seg);
-    const int64_t grid = (int64_t)a.BH * ((max_n + KEYS - 1) / KEYS) * a.n_seg;
+    const int64_t grid = (int64_t)a.BH * ((max_n + kMassKeys - 1) / kMassKeys) * a.n_seg;
     if (grid >= (int64_t)1 << 31) return SOCKET_EUNSUPPORTED;
     hipLaunchKernelGGL((key_mass_kernel<T, D, CAP, BIAS>), dim3((unsigned)grid), dim3(kMassThreads), 0, st, a);
-    if (a.n_seg > 1) hipLaunchKernelGGL((key_mass_merge_kernel<KEYS, Tile::QT>), dim3((unsigned)((max_n + 255) / 256) * (unsigned)a.BH), dim3(256), 0, st, a);
+    if (a.n_seg > 1) hipLaunchKernelGGL((key_mass_merge_kernel<Tile::QT>), dim3((unsigned)((max_n + 255) / 256) * (unsigned)a.BH), dim3(256), 0, st, a);
     return SOCKET_OK;
 }
 
