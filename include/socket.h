@@ -407,6 +407,7 @@ int socket_key_mass(socket_ctx *ctx, const void *q, const void *K, const float *
  * others, but its token can be kept, so that every head keeps the same number.  Writes the ranking into
  * scores ([B, Hkv, max_n] float32, not the array of masses), then idx and n_selected as
  * socket_topk_select does.  Like that call it discards a pending socket_score_keys_binned.
+ * mass and scores have to be aligned to 16 bytes.
  * seq_len, keep: device int32 [batch]; keep[b] is clamped to max_k.
  */
 int socket_evict_select(socket_ctx *ctx, const float *mass, const int32_t *block_table, const int32_t *seq_len,

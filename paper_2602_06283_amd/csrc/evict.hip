@@ -10,7 +10,8 @@ namespace sk {
 
 // ---- scores: the mass, pooled over the tokens around (the largest of pool of them); +inf for the
 //      tokens that are always kept, -inf behind the sequence and where there is no block
-constexpr int kPoolThreads = 256;
+//      Bound by latency on one sequence, by the 8 bytes a token on many: four tokens a thread.
+constexpr int kPoolThreads = 256, kPoolTokens = 4 * kPoolThreads, kPoolMax = 255;
 
 struct EvictScoreArgs {
     const float *mass;
@@ -21,34 +22,57 @@ struct EvictScoreArgs {
 };
 
 __global__ __launch_bounds__(kPoolThreads) void evict_scores_kernel(EvictScoreArgs a) {
-    __shared__ float s_x[kPoolThreads + 256];
+    constexpr int HALO = (kPoolMax / 2 + 3) / 4 * 4;
+    __shared__ __align__(16) float s_x[kPoolTokens + 2 * HALO];  // masses from HALO tokens before the first
+    __shared__ int s_gone[kPoolTokens / 16];
     const int tid = threadIdx.x, h = blockIdx.y, b = blockIdx.z, side = a.pool / 2;
-    const int t0 = blockIdx.x * kPoolThreads, t = t0 + tid;
+    const int t0 = blockIdx.x * kPoolTokens, t = t0 + 4 * tid;
     const int64_t row = ((int64_t)b * a.map.Hkv + h) * a.map.max_n;
     const int len = min(a.seq_len[b], a.map.max_n);
-    const float ninf = -__builtin_inff();
-    if (t0 >= len) {
-        if (t < a.map.max_n) a.scores[row + t] = ninf;
-        return;
-    }
-    for (int o = tid; o < kPoolThreads + 2 * side; o += kPoolThreads) {
-        const int u = t0 - side + o;
-        float x = ninf;
-        if (u >= 0 && u < len) {
-            x = a.mass[row + u];
-            x = x >= -3.4028234663852886e38f ? x : -3.4028234663852886e38f;   // (NaN and -inf: the last to be kept)
+    const float ninf = -__builtin_inff(), least = -3.4028234663852886e38f;
+    // (max_n is a multiple of 16: a thread's four tokens are all inside it or all behind it)
+    f32x4_t s = {ninf, ninf, ninf, ninf};
+    if (t0 < len) {
+        auto clean = [&](float x) { return x >= least ? x : least; };        // (NaN and -inf: the last to be kept)
+        f32x4_t own = s;
+        if (t < len) own = *(const f32x4_t *)&a.mass[row + t];               // (whole: len <= max_n)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) own[e] = t + e < len ? clean(own[e]) : ninf;
+        *(f32x4_t *)&s_x[HALO + 4 * tid] = own;
+        if (tid < 2 * side) {
+            const int u = tid < side ? t0 - side + tid : t0 + kPoolTokens + tid - side;
+            s_x[HALO + u - t0] = u >= 0 && u < len ? clean(a.mass[row + u]) : ninf;
         }
-        s_x[o] = x;
+        if (a.map.block_table && tid < kPoolTokens / 16) {
+            const int u = t0 + 16 * tid;
+            s_gone[tid] = u < len && a.map.row(b, h, u) < 0;
+        }
+        __syncthreads();
+        s = own;
+        if (side && side <= 4) {                     // the four tokens before and the four behind, 16 bytes each
+            const f32x4_t left = *(const f32x4_t *)&s_x[HALO + 4 * tid - 4], right = *(const f32x4_t *)&s_x[HALO + 4 * tid + 4];
+            const float x[12] = {left.x, left.y, left.z, left.w, own.x, own.y, own.z, own.w, right.x, right.y, right.z, right.w};
+#pragma unroll
+            for (int o = 1; o <= 4; ++o) {
+                if (o > side) break;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[e] = fmaxf(s[e], fmaxf(x[4 + e - o], x[4 + e + o]));
+            }
+        } else if (side) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const float *x = &s_x[HALO + 4 * tid + e - side];
+                for (int o = 0; o < a.pool; ++o) s[e] = fmaxf(s[e], x[o]);
+            }
+        }
+        const bool gone = a.map.block_table && s_gone[tid / 4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            if (t + e < a.n_sink || t + e >= len - a.n_window) s[e] = __builtin_inff();
+            if (t + e >= len || gone) s[e] = ninf;
+        }
     }
-    __syncthreads();
-    if (t >= a.map.max_n) return;
-    float s = ninf;
-    if (t < len) {
-        for (int o = 0; o < a.pool; ++o) s = fmaxf(s, s_x[tid + o]);
-        if (t < a.n_sink || t >= len - a.n_window) s = __builtin_inff();
-        if (a.map.row(b, h, t) < 0) s = ninf;
-    }
-    a.scores[row + t] = s;
+    if (t < a.map.max_n) *(f32x4_t *)&a.scores[row + t] = s;
 }
 
 // ---- moving rows
@@ -280,7 +304,7 @@ int launch_evict_scores(socket_ctx *ctx, const float *mass, const int32_t *block
     a.mass = mass; a.scores = scores; a.seq_len = seq_len;
     a.map = row_map(g, block_table);
     a.pool = pool; a.n_sink = ctx->n_sink; a.n_window = ctx->n_window;
-    hipLaunchKernelGGL(evict_scores_kernel, dim3((g.max_n + kPoolThreads - 1) / kPoolThreads, g.Hkv, batch), dim3(kPoolThreads), 0, st, a);
+    hipLaunchKernelGGL(evict_scores_kernel, dim3((g.max_n + kPoolTokens - 1) / kPoolTokens, g.Hkv, batch), dim3(kPoolThreads), 0, st, a);
     return record_hip(ctx, hipGetLastError());
 }
 

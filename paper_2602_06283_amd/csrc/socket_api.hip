@@ -434,7 +434,7 @@ int socket_evict_select(socket_ctx *ctx, const float *mass, const int32_t *block
                         int32_t *n_selected, void *stream) {
     if (!ctx || !mass || !seq_len || !keep || !scores || !idx || !n_selected) return SOCKET_EINVAL;
     if (!batch_ok(ctx, batch) || !paging_ok(ctx, block_table)) return SOCKET_EINVAL;
-    if (pool < 1 || pool > 255 || pool % 2 == 0 || mass == scores) return SOCKET_EINVAL;
+    if (pool < 1 || pool > 255 || pool % 2 == 0 || mass == scores || !aligned16({mass, scores})) return SOCKET_EINVAL;
     int rc = drop_pending(ctx, (hipStream_t)stream);
     if (rc != SOCKET_OK) return rc;
     rc = launch_evict_scores(ctx, mass, block_table, seq_len, batch, pool, scores, (hipStream_t)stream);

@@ -25,7 +25,7 @@ def wanted(mass, length, keep, pool, sink, window, absent=None):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("pool", [1, 3, 7, 255])
+@pytest.mark.parametrize("pool", [1, 3, 7, 11, 255])
 @pytest.mark.parametrize("n,page", [(16, 0), (1008, 48), (5008, 0), (50000, 16)])
 def test_select_keeps_the_largest_masses(n, page, pool):
     rng = np.random.default_rng(n + pool)
