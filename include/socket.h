@@ -420,10 +420,10 @@ int socket_evict_select(socket_ctx *ctx, const float *mass, const int32_t *block
  * the new position), value norm and mass.  The sequence is n_selected tokens long afterwards; rows
  * behind that are left as they were.  Entries of idx outside [0, max_n), and tokens or new positions whose
  * block is absent, are skipped.
- * In place when a cache and its _out are the same tensor under the same block table (give the
- * same pointer for both); idx then has to ascend strictly, as the selects write it, and paged
- * sequences must not share blocks.  Otherwise no _out may overlap a source: other tensors, or, paged, blocks
- * of the same pools that no source sequence uses.  vnorm and mass may be in place in either case.
+ * A cache and its _out may be the same tensor: in place, or, paged, with a block_table_out that
+ * gives every sequence either the blocks it has or others that no sequence uses.  idx then has to ascend strictly, as
+ * the selects write it, and no two sequences may share a block that one of them moves rows within.
+ * Otherwise no _out may overlap a source.
  * codes, vnorm and mass: NULL together with their _out.  K, V, codes and their _outs have to be
  * aligned to 16 bytes.
  */

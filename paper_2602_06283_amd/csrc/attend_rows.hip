@@ -1003,7 +1003,7 @@ int launch_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void
         a.n_tiles = two && !wide ? 2 : 1;
         a.n_split = pick_splits(8192 / (a.BH * a.n_tiles), (g.max_n + 31) / 32, room);
         const int64_t grid = (int64_t)a.BH * a.n_tiles * a.n_split;
-        if (grid >= (int64_t)1 << 31) return SOCKET_EUNSUPPORTED;
+        if (grid * 64 >= (int64_t)1 << 32) return SOCKET_EUNSUPPORTED;       // (threads of a launch)
         const dim3 gr((unsigned)grid);
         switch (g.d) {
             case 64: f32 ? launch_few<float, 64>(a, wide, gr, st) : launch_few<uint16_t, 64>(a, wide, gr, st); break;
@@ -1012,13 +1012,14 @@ int launch_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void
             default: return SOCKET_EUNSUPPORTED;
         }
     } else {
-        // Two workgroups per compute unit keep it busy; with fewer the keys are split, down to four tiles each
-        // and as far as the partial results fit.
+        // Two workgroups per compute unit keep it busy; with fewer the keys are split, 512 or more to a split and
+        // as far as the partial results fit (256: 512 prompt rows 23 us with the launch that joins them, 18 without;
+        // half as many splits: 256 rows behind 32000 245 us instead of 180).
         a.n_tiles = (int)(((int64_t)max_rows * g.G + kRowsQueries - 1) / kRowsQueries);
         const int64_t wgs = (int64_t)a.BH * a.n_tiles;
-        a.n_split = pick_splits(512 / wgs, (g.max_n + 255) / 256, room);
+        a.n_split = pick_splits(512 / wgs, (g.max_n + 511) / 512, room);
         const int64_t grid = wgs * a.n_split;
-        if (grid >= (int64_t)1 << 31) return SOCKET_EUNSUPPORTED;
+        if (grid * kRowsThreads >= (int64_t)1 << 32) return SOCKET_EUNSUPPORTED;
         const dim3 gr((unsigned)grid);
         switch (g.d) {
             case 64: f32 ? launch_rows<float, 64>(a, gr, st) : launch_rows<uint16_t, 64>(a, gr, st); break;

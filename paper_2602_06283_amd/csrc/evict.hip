@@ -214,7 +214,7 @@ __global__ __launch_bounds__(kMoveThreads) void evict_move_kernel(MoveArgs a) {
     }
 }
 
-// In place.  Entry j of an ascending index row lies at position j or behind it, so rows that are
+// In place, or within the same pools.  Entry j of an ascending index row lies at position j or behind it, so rows that are
 // moved in order never land on one that is still to be read; a workgroup takes a slice of the row's
 // bytes of one head, reads a pass of rows into registers, and writes them once all of the pass are
 // there.  Slices of 64 bytes: what one head's move can be shared out in.
@@ -327,7 +327,9 @@ int launch_evict_rows(socket_ctx *ctx, const int32_t *idx, const int32_t *n_sele
     a.dst = row_map(g, block_table_out);
     a.max_k = g.max_k; a.Lpad = g.Lpad; a.GT = g.GT; a.strings = g.Lpad / 16; a.cb = g.cb;
     const int rowb = g.d * (g.kv_dtype == SOCKET_F32 ? 4 : 2);
-    const bool in_place = block_table == block_table_out && (K == K_out || V == V_out || (codes && codes == codes_out));
+    // (the same pools under another table may be in place all the same, if the tables say the same: moving in
+    // order is right then, and where the blocks are others)
+    const bool in_place = K == K_out || V == V_out || (codes && codes == codes_out);
     // (the float arrays are by sequence, not by block: they can be in place where the caches are not)
     const bool vnorm_ordered = vnorm && (in_place || vnorm == vnorm_out), mass_ordered = mass && (in_place || mass == mass_out);
     if (!in_place) {

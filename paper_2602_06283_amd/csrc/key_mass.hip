@@ -421,7 +421,8 @@ template <typename T, int D, bool CAP, bool BIAS> static int launch_mass_tiles(M
     a.n_seg = seg < 1 ? 1 : (int)seg;
     a.seg_tiles = (int)((tiles + a.n_seg - 1) / a.n_seg);
     const int64_t grid = (int64_t)a.BH * ((max_n + kMassKeys - 1) / kMassKeys) * a.n_seg;
-    if (grid >= (int64_t)1 << 31) return SOCKET_EUNSUPPORTED;
+    // (threads of a launch; a tile's rows lie within 32 bits of each other)
+    if (grid * kMassThreads >= (int64_t)1 << 32 || (int64_t)a.Hq * Tile::ROWB * Tile::QT >= (int64_t)1 << 31) return SOCKET_EUNSUPPORTED;
     hipLaunchKernelGGL((key_mass_kernel<T, D, CAP, BIAS>), dim3((unsigned)grid), dim3(kMassThreads), 0, st, a);
     if (a.n_seg > 1) hipLaunchKernelGGL((key_mass_merge_kernel<Tile::QT>), dim3((unsigned)((max_n + 255) / 256) * (unsigned)a.BH), dim3(256), 0, st, a);
     return SOCKET_OK;
@@ -435,7 +436,7 @@ template <typename T, int D> static int launch_mass(MassArgs a, int64_t room, in
         n = n < most ? n : most;
         a.n_seg = n < 1 ? 1 : (int)n;
         const int64_t grid = (int64_t)a.BH * a.n_seg;
-        if (grid >= (int64_t)1 << 31) return SOCKET_EUNSUPPORTED;
+        if (grid * 64 >= (int64_t)1 << 32) return SOCKET_EUNSUPPORTED;       // (threads of a launch)
         if ((int64_t)rows * a.G > 16) hipLaunchKernelGGL((key_mass_few_kernel<T, D, 2>), dim3((unsigned)grid), dim3(64), 0, st, a);
         else hipLaunchKernelGGL((key_mass_few_kernel<T, D, 1>), dim3((unsigned)grid), dim3(64), 0, st, a);
         return SOCKET_OK;

@@ -36,6 +36,8 @@ def test_select_keeps_the_largest_masses(n, page, pool):
     mass[0, 0, rng.integers(0, n, n // 3)] = 0.25                # many equal
     mass[1, 0, 5], mass[1, 1, 3], mass[1, 1, 7] = math.nan, -math.inf, math.inf
     lens, keep = [n, n - 3, 1, 0], [k, k // 2, k, k]
+    if pool == 3:
+        keep[1] = 0
     table, absent = None, None
     if page:
         table = rng.permutation(B * blocks).reshape(B, blocks).astype(np.int32)
@@ -159,6 +161,15 @@ def test_move_in_place_over_many_passes():
         same = (c.K, c.V, c.codes, c.norms, c.mass)
         c.move(same, c.table, c.table)
         c.check(before, c.all(same, c.table), before)
+
+
+@pytest.mark.gpu
+def test_move_in_place_under_a_copy_of_the_block_table():
+    c = Cache(17, 64, 8, B=1, Hkv=2, n=6000, page=48, k=5001)
+    before = c.all((c.K, c.V, c.codes, c.norms, c.mass), c.table)
+    same = (c.K, c.V, c.codes, c.norms, c.mass)
+    c.move(same, c.table, c.table.clone())
+    c.check(before, c.all(same, c.table), before)
 
 
 @pytest.mark.gpu
