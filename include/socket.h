@@ -375,7 +375,8 @@ typedef struct socket_attn_mods {
  * Rows behind row_count[b] are left as they were.  A row that sees no key gives zeros and
  * lse = -inf, and so does one whose scores all are -inf.  Keys and values that a row does not see
  * never count, infinities and NaN included.  q, K, V and out have to be aligned to 16 bytes.
- * bf16 caches: fp32 sums; the softmax weights are rounded to bf16 once where out is bf16.
+ * bf16 caches: fp32 sums; where out is bf16 and max_rows Hq/Hkv is above 32, the softmax weights are
+ * rounded to bf16 once.
  * row_begin, row_count: device int32 [batch].
  */
 int socket_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void *V, const int32_t *block_table,

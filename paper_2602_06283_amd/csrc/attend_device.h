@@ -198,15 +198,36 @@ template <> __device__ __forceinline__ void mma_piece<float>(floatx16_t &c, u32x
 // the same for tiles of 16 rows (lane = column lane % 16; sixteenth of the wavefront g = lane / 16): a
 // k-step of bf16 takes piece 4 c + g, four k-steps of fp32 do
 typedef float floatx4v_t __attribute__((ext_vector_type(4)));
-template <typename T> __device__ __forceinline__ void mma_piece16(floatx4v_t &c, u32x4_t a, u32x4_t b);
-template <> __device__ __forceinline__ void mma_piece16<uint16_t>(floatx4v_t &c, u32x4_t a, u32x4_t b) {
-    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v_t, a), __builtin_bit_cast(bf16x8v_t, b), c, 0, 0, 0);
+__device__ __forceinline__ floatx4v_t mma16(u32x4_t a, u32x4_t b, floatx4v_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8v_t, a), __builtin_bit_cast(bf16x8v_t, b), c, 0, 0, 0);
 }
-template <> __device__ __forceinline__ void mma_piece16<float>(floatx4v_t &c, u32x4_t a, u32x4_t b) {
-    const f32x4_t x = __builtin_bit_cast(f32x4_t, a), y = __builtin_bit_cast(f32x4_t, b);
+
+// In fp32 the four k-steps of a piece have a sum each, added up at the end: four short chains of
+// additions round less than a long one (twelve outputs over 4096 fp32 keys, d = 128: 3.6e-7 off at most, 1.6e-6 with one).
+template <typename T> struct Tile16;
+template <> struct Tile16<uint16_t> {
+    floatx4v_t c = 0.0f;
+    __device__ __forceinline__ void add(u32x4_t a, u32x4_t b) {
+        c = mma16(a, b, c);
+    }
+    __device__ __forceinline__ floatx4v_t total() const { return c; }
+};
+template <> struct Tile16<float> {
+    floatx4v_t c0 = 0.0f, c1 = 0.0f, c2 = 0.0f, c3 = 0.0f;
+    __device__ __forceinline__ void add(u32x4_t a, u32x4_t b) {
+        const f32x4_t x = __builtin_bit_cast(f32x4_t, a), y = __builtin_bit_cast(f32x4_t, b);
+        c0 = __builtin_amdgcn_mfma_f32_16x16x4f32(x[0], y[0], c0, 0, 0, 0);
+        c1 = __builtin_amdgcn_mfma_f32_16x16x4f32(x[1], y[1], c1, 0, 0, 0);
+        c2 = __builtin_amdgcn_mfma_f32_16x16x4f32(x[2], y[2], c2, 0, 0, 0);
+        c3 = __builtin_amdgcn_mfma_f32_16x16x4f32(x[3], y[3], c3, 0, 0, 0);
+    }
+    __device__ __forceinline__ floatx4v_t total() const {
+        floatx4v_t t;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
-}
+        for (int e = 0; e < 4; ++e) t[e] = (c0[e] + c1[e]) + (c2[e] + c3[e]);
+        return t;
+    }
+};
 
 // max over the four sixteenths of a wavefront
 __device__ __forceinline__ float sixteenths_max(float v) {

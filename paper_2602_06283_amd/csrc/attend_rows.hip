@@ -11,8 +11,10 @@
 // the lower lanes, 4-7 and 12-15 for the upper), so they never leave their lanes.
 //
 // bf16 caches: products of bf16 with fp32 sums.  The weights are rounded once to bf16 where the
-// output is bf16 (half a step each, as the output's own rounding); where the output is fp32 they
-// go in as three bf16 pieces, which hold all 24 bits.  fp32 caches: fp32 matrix instructions.
+// output is bf16 (half a step each, as the output's own rounding; two pieces, 17 bits, would cost the matrix
+// units half as much again), except that few rows, which wait for memory, take two pieces for the
+// same time; where the output is fp32 they go in as three, which hold all 24 bits.  fp32 caches:
+// fp32 matrix instructions.
 //
 // Few rows: the keys are split over workgroups, whose (maximum, sum, weighted values) a second
 // launch joins, split by split in a fixed order.
@@ -183,10 +185,13 @@ template <int D, int PX> struct ValueStages<float, D, PX> {
         w[e + 1] = p1;
     }
     static __device__ __forceinline__ Part read(const char *v, int stage, int lane) {
-        const int row = 32 * (stage / 16) + tile_row(stage % 16, lane >> 5), ch = lane & 31;
+        // channel 32 cb + lane % 32 of row tile_row: v_piece, with the lane's part apart, which is one of two (the
+        // compiler keeps an address of its own for every read otherwise, 157 registers too many at d = 256)
+        const int hf = lane >> 5, at = 4 * hf * Tile::ROWB + 4 * (lane & 31), side[2] = {at + 128 * hf, at + 128 * (1 - hf)};
+        const int row = 32 * (stage / 16) + tile_row(stage % 16, 0);
         Part part;
 #pragma unroll
-        for (int cb = 0; cb < D / 32; ++cb) part.v[cb] = *(const float *)(v + Tile::v_piece(row, 8 * cb + (ch >> 2)) * 16 + (ch & 3) * 4);
+        for (int cb = 0; cb < D / 32; ++cb) part.v[cb] = *(const float *)(v + side[cb & 1] + row * Tile::ROWB + 256 * (cb / 2));
         return part;
     }
     __device__ __forceinline__ void add(floatx16_t (&o)[D / 32], int stage, const Part &part) const {
@@ -334,6 +339,11 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D 
     // constants differs between the logits: their sums with it were kept in registers otherwise, one each.)
     auto key_row = [](int e) __attribute__((always_inline)) { return 32 * (e / 16) + tile_row(e % 16, 0); };
     const int i_lane = i - 4 * hf - base;
+    // fp32 tiles go one part after the other: an instruction keeps its matrix unit busy for 64 cycles, next to which
+    // the softmax is little, and the registers of two tiles' logits are spared (2011 rows of 8 heads, d = 64, 33.7 us
+    // in the order of the bf16 ones, 30.5 in this; 2048 rows, d = 256, 235 and 224).  A scheduling barrier ends each
+    // read and its products: reads that all go first take their registers together.
+    constexpr bool SERIAL = sizeof(T) == 4;
     auto read_k = [&](const char *kt, int ks, u32x4_t (&f)[NU]) __attribute__((always_inline)) {
 #pragma unroll
         for (int u = 0; u < NU; ++u) f[u] = *(const u32x4_t *)(kt + Tile::k_piece(32 * u + (lane & 31), 2 * ks + hf) * 16);
@@ -347,6 +357,7 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D 
             read_k(kt, ks, f);
 #pragma unroll
             for (int u = 0; u < NU; ++u) mma_piece<T>(s[u], f[u], q[ks]);
+            if (SERIAL) __builtin_amdgcn_sched_barrier(0);
         }
     };
     auto across = [&](float x) __attribute__((always_inline)) {              // the larger of the two halves'
@@ -416,6 +427,31 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(D 
         if (tile + 2 < t_end) load_k(tile + 2, k_to);
         const bool was_seen = seen;
         seen = tile + 1 < t_end && sees(tile + 1);
+        if constexpr (SERIAL) {
+            if (was_seen) {
+                float part = 0.0f;
+#pragma unroll
+                for (int e = 0; e < E; e += 2) {
+                    const float p0 = exp2_fast(s[e / 16][e % 16]), p1 = exp2_fast(s[e / 16][e % 16 + 1]);
+                    part += p0 + p1;
+                    values.set(e, p0, p1);
+                }
+                sum += part;
+#pragma unroll
+                for (int st = 0; st < Values::COUNT; ++st) {
+                    const typename Values::Part part_v = Values::read(v_now, st, lane);
+                    values.add(o, st, part_v);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            if (seen) {
+                products(k_next, s);
+                const LogitOf<CAP, BIAS> logit(a.mods, (float)(i_lane - (tile + 1) * KT), slope2, top == ninf ? 0.0f : top);
+#pragma unroll
+                for (int e = 0; e < E; ++e) s[e / 16][e % 16] = logit.any(s[e / 16][e % 16], key_row(e));
+                settle(tile + 1, s, largest(s));
+            }
+        } else
         if (was_seen || seen) {                      // (neither: the logits are -inf, and stay it)
 #pragma unroll
         for (int ks = 0; ks < AHEAD; ++ks) read_k(k_next, ks, fk[ks]);
@@ -676,23 +712,23 @@ __global__ __launch_bounds__(64) void attend_few_kernel(RowsArgs a) {
         // ---- logits
         float s[NQ][4 * NT];
         {
-            floatx4v_t c[NQ][NT];
-#pragma unroll
-            for (int x = 0; x < NQ; ++x)
-#pragma unroll
-                for (int t = 0; t < NT; ++t) c[x][t] = 0.0f;
+            Tile16<T> c[NQ][NT];
 #pragma unroll
             for (int ks = 0; ks < NKS; ++ks)
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     const u32x4_t kf = *(const u32x4_t *)(kt + Tile::k_piece(16 * t + (lane & 15), 4 * ks + g) * 16);
 #pragma unroll
-                    for (int x = 0; x < NQ; ++x) mma_piece16<T>(c[x][t], kf, q[x][ks]);
+                    for (int x = 0; x < NQ; ++x) c[x][t].add(kf, q[x][ks]);
                 }
 #pragma unroll
             for (int x = 0; x < NQ; ++x)
 #pragma unroll
-                for (int e = 0; e < 4 * NT; ++e) s[x][e] = c[x][e / 4][e % 4];
+                for (int t = 0; t < NT; ++t) {
+                    const floatx4v_t dots = c[x][t].total();
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[x][4 * t + e] = dots[e];
+                }
         }
 #pragma unroll
         for (int x = 0; x < NQ; ++x) {
@@ -752,7 +788,7 @@ __global__ __launch_bounds__(64) void attend_few_kernel(RowsArgs a) {
 #pragma unroll
                 for (int x = 0; x < NQ; ++x)
 #pragma unroll
-                    for (int y = 0; y < PX; ++y) mma_piece16<uint16_t>(o[x][cb], f.v, w[x][y]);
+                    for (int y = 0; y < PX; ++y) o[x][cb] = mma16(f.v, w[x][y], o[x][cb]);
             }
         } else {
 #pragma unroll
@@ -965,7 +1001,7 @@ template <typename T, int D> static void launch_few(const RowsArgs &a, bool wide
     if constexpr (sizeof(T) == 2) {
         if (a.out_dtype == SOCKET_F32) return launch_few<T, D, 3>(a, wide, grid, st);
     }
-    launch_few<T, D, 1>(a, wide, grid, st);
+    launch_few<T, D, sizeof(T) == 2 ? 2 : 1>(a, wide, grid, st);
 }
 
 template <int D> static void launch_rows_merge(const RowsArgs &a, bool few, int items, dim3 grid, hipStream_t st) {
@@ -1012,12 +1048,19 @@ int launch_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void
             default: return SOCKET_EUNSUPPORTED;
         }
     } else {
-        // Two workgroups per compute unit keep it busy; with fewer the keys are split, 512 or more to a split and
-        // as far as the partial results fit (256: 512 prompt rows 23 us with the launch that joins them, 18 without;
-        // half as many splits: 256 rows behind 32000 245 us instead of 180).
+        // Two workgroups per compute unit keep it busy (one at d = 256, where one fits); with fewer the keys are split,
+        // as far as the partial results fit (half as many splits: 256 rows behind 32000 245 us instead of 180).  Where
+        // the run is most of the cache its first rows see few keys and its last ones many, and twice as many even that
+        // out (4096 fp32 rows of 8 heads 455 -> 340 us, 8192 bf16 rows of 8 heads 221 -> 200; but 2048 rows behind
+        // 16384 179 -> 197; at d = 256 four to a compute unit: 2048 fp32 rows of 8 heads 195 -> 230).
+        // A split's products have to be worth the results it leaves: 512 keys and more in bf16 (256: 512 prompt rows
+        // 23 us with the launch that joins them, 18 without); in fp32 they take longer the wider the heads (512 at
+        // d = 64: 256 there 33 -> 42 us for 2011 rows; 256 at d = 128: 1024 rows 97 -> 59; 128 at d = 256: 300 rows
+        // 54 -> 46).
         a.n_tiles = (int)(((int64_t)max_rows * g.G + kRowsQueries - 1) / kRowsQueries);
         const int64_t wgs = (int64_t)a.BH * a.n_tiles;
-        a.n_split = pick_splits(512 / wgs, (g.max_n + 511) / 512, room);
+        const int wanted = (2 * (int64_t)max_rows >= g.max_n ? 1024 : 512) / (g.d == 256 ? 2 : 1), least = f32 ? 32768 / g.d : 512;
+        a.n_split = pick_splits(wanted / wgs, (g.max_n + least - 1) / least, room);
         const int64_t grid = wgs * a.n_split;
         if (grid * kRowsThreads >= (int64_t)1 << 32) return SOCKET_EUNSUPPORTED;
         const dim3 gr((unsigned)grid);

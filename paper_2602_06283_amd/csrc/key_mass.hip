@@ -367,17 +367,13 @@ __global__ __launch_bounds__(64) void key_mass_few_kernel(MassArgs a) {
     for (int tile = t_begin; tile < t_end; ++tile) {
         const int t0 = tile * KT, gone = gone_next;
         const float old = old_next;
-        floatx4v_t c[NQ][NT];
-#pragma unroll
-        for (int x = 0; x < NQ; ++x)
-#pragma unroll
-            for (int y = 0; y < NT; ++y) c[x][y] = 0.0f;
+        Tile16<T> c[NQ][NT];
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks)
 #pragma unroll
             for (int y = 0; y < NT; ++y)
 #pragma unroll
-                for (int x = 0; x < NQ; ++x) mma_piece16<T>(c[x][y], kn[y][ks], q[x][ks]);
+                for (int x = 0; x < NQ; ++x) c[x][y].add(kn[y][ks], q[x][ks]);
         if (tile + 1 < t_end) {
             load(tile + 1);
             look_up(tile + 2);
@@ -389,7 +385,11 @@ __global__ __launch_bounds__(64) void key_mass_few_kernel(MassArgs a) {
         for (int x = 0; x < NQ; ++x) {
             float s[4 * NT];
 #pragma unroll
-            for (int e = 0; e < 4 * NT; ++e) s[e] = c[x][e / 4][e % 4];
+            for (int y = 0; y < NT; ++y) {
+                const floatx4v_t dots = c[x][y].total();
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[4 * y + e] = dots[e];
+            }
             logits2(a.mods, s, (float)(run.begin + ((first_m + 16 * x + (lane & 15)) >> a.g_log2) - 4 * g - t0), slope2[x], lse[x],
                     [](int e) { return 16 * (e / 4) + e % 4; });
             const uint32_t span = lo[x] <= hi[x] ? (uint32_t)(hi[x] - lo[x]) : 0u;

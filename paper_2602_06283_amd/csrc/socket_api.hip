@@ -207,9 +207,9 @@ int socket_create(socket_ctx **out, const socket_params *p) {
     const int64_t sz_staged = BH * g.max_k * 4;
     const int64_t sz_regions = BH * g.n_regions * kSlice * 4, sz_selcnt = BH * g.n_regions * 4;
     const int64_t sz_seq = (int64_t)g.max_batch * 4;
-    // (runs of rows split their keys as far as this holds the partial results: 32 MiB are 31 splits of 64
-    // rows of 32 query heads, d = 128)
-    const int64_t sz_part = std::max((int64_t)g.max_batch * g.Hq * kMaxSplits * (g.d + 2) * 4, (int64_t)32 << 20);
+    // (runs of rows split their keys as far as this holds the partial results: 128 MiB are seven splits of
+    // 4096 rows of 8 query heads, d = 128; with 32 MiB, one, they took 664 us in fp32 instead of 340)
+    const int64_t sz_part = std::max((int64_t)g.max_batch * g.Hq * kMaxSplits * (g.d + 2) * 4, (int64_t)128 << 20);
     ctx->partial_floats = sz_part / 4;
     ctx->scratch_bytes = sz_tables + sz_tstats + sz_sub + sz_hist + sz_cnt + 2 * sz_cand + sz_staged + sz_regions + sz_selcnt + sz_part + sz_seq;
     bool ok = score_prepare(g) == SOCKET_OK &&
