@@ -42,7 +42,7 @@ __device__ __forceinline__ float kept_mass(const MassArgs &a, const RowRun &run,
 // ---- many queries: a workgroup's four wavefronts own 32 keys each and share the queries, 64 at a time, in
 //      two LDS buffers that are filled straight from memory.  (64 keys each read half as much of LDS, but their
 //      registers leave room for two wavefronts a SIMD, not three: 4096 rows 128 us against 118.)  Long runs are cut into
-//      segments of 16 tiles, whose sums a second launch adds up: the first keys of a prompt are seen by all of
+//      segments, whose sums a second launch adds up: the first keys of a prompt are seen by all of
 //      its rows, the last by few, and with segments no workgroup has more to do than another.
 constexpr int kMassThreads = 256, kMassKeys = 128;
 
@@ -415,12 +415,18 @@ __global__ __launch_bounds__(64) void key_mass_few_kernel(MassArgs a) {
 template <typename T, int D, bool CAP, bool BIAS> static int launch_mass_tiles(MassArgs a, int64_t room, int max_n, int rows, hipStream_t st) {
     using Tile = MassTile<T, D>;
     const int64_t tiles = ((int64_t)rows * a.G + Tile::QT - 1) / Tile::QT;
-    int64_t seg = (tiles + 15) / 16;
+    const int64_t keys = (int64_t)a.BH * ((max_n + kMassKeys - 1) / kMassKeys), most = (tiles + 3) / 4;
+    // segments of 16 tiles; shorter ones, four tiles at least, where that is fewer than four workgroups to a compute
+    // unit, or eight where the run is most of the cache and half of the workgroups see nothing (500 rows of 32 heads
+    // 25 -> 13 us, 4096 fp32 rows of 8 heads 273 -> 214; eight everywhere: four runs of 100 rows behind 2000 18 -> 24)
+    const int64_t more = (2 * (int64_t)rows >= max_n ? 2048 : 1024) / keys;
+    int64_t seg = more < most ? more : most;
+    seg = seg > (tiles + 15) / 16 ? seg : (tiles + 15) / 16;
     const int64_t fits = room / ((int64_t)a.BH * max_n);
     seg = seg < fits ? seg : fits;
     a.n_seg = seg < 1 ? 1 : (int)seg;
     a.seg_tiles = (int)((tiles + a.n_seg - 1) / a.n_seg);
-    const int64_t grid = (int64_t)a.BH * ((max_n + kMassKeys - 1) / kMassKeys) * a.n_seg;
+    const int64_t grid = keys * a.n_seg;
     // (threads of a launch; a tile's rows lie within 32 bits of each other)
     if (grid * kMassThreads >= (int64_t)1 << 32 || (int64_t)a.Hq * Tile::ROWB * Tile::QT >= (int64_t)1 << 31) return SOCKET_EUNSUPPORTED;
     hipLaunchKernelGGL((key_mass_kernel<T, D, CAP, BIAS>), dim3((unsigned)grid), dim3(kMassThreads), 0, st, a);
