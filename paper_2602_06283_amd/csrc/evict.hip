@@ -10,7 +10,8 @@ namespace sk {
 
 // ---- scores: the mass, pooled over the tokens around (the largest of pool of them); +inf for the
 //      tokens that are always kept, -inf behind the sequence and where there is no block
-//      Bound by latency on one sequence, by the 8 bytes a token on many: four tokens a thread.
+//      Bound by latency on one sequence (32768 tokens of 8 heads, pool 5: 3.8 us), by the 8 bytes a token on many
+//      (16 ragged paged sequences 5.4 us; a token a thread 9.4): four tokens a thread.
 constexpr int kPoolThreads = 256, kPoolTokens = 4 * kPoolThreads, kPoolMax = 255;
 
 struct EvictScoreArgs {
@@ -29,11 +30,12 @@ __global__ __launch_bounds__(kPoolThreads) void evict_scores_kernel(EvictScoreAr
     const int t0 = blockIdx.x * kPoolTokens, t = t0 + 4 * tid;
     const int64_t row = ((int64_t)b * a.map.Hkv + h) * a.map.max_n;
     const int len = min(a.seq_len[b], a.map.max_n);
-    const float ninf = -__builtin_inff(), least = -3.4028234663852886e38f;
+    const float ninf = -__builtin_inff(), most = 3.4028234663852886e38f;
     // (max_n is a multiple of 16: a thread's four tokens are all inside it or all behind it)
     f32x4_t s = {ninf, ninf, ninf, ninf};
     if (t0 < len) {
-        auto clean = [&](float x) { return x >= least ? x : least; };        // (NaN and -inf: the last to be kept)
+        // (NaN and -inf: the last to be kept; +inf: behind the tokens that are always kept)
+        auto clean = [&](float x) { return x >= -most ? fminf(x, most) : -most; };
         f32x4_t own = s;
         if (t < len) own = *(const f32x4_t *)&a.mass[row + t];               // (whole: len <= max_n)
 #pragma unroll
@@ -160,7 +162,8 @@ template <int CB> struct IdString {
     }
 };
 
-// To other tensors or blocks: every row by itself, 32 rows a workgroup.
+// To other tensors or blocks: every row by itself, 32 rows a workgroup.  (4096 of 32768 tokens of 8 heads 6.5 us;
+// 16 paged sequences, 1001 tokens of each head, ids of 10 bits, 20 us.)
 constexpr int kMoveThreads = 256, kMoveRows = 32;
 
 template <int ROWB, int CB>

@@ -15,7 +15,7 @@ def wanted(mass, length, keep, pool, sink, window, absent=None):
     """Positions kept of one row of masses, ascending."""
     n = max(0, min(length, len(mass)))
     x = mass[:n].astype(np.float64)
-    x = np.where(x >= np.finfo(np.float32).min, x, np.finfo(np.float32).min)
+    x = np.where(x >= np.finfo(np.float32).min, np.minimum(x, np.finfo(np.float32).max), np.finfo(np.float32).min)
     y = np.array([x[max(0, t - pool // 2):t + pool // 2 + 1].max() for t in range(n)])
     y[:sink] = np.inf
     y[max(0, n - window):] = np.inf
@@ -206,6 +206,19 @@ def test_entries_and_blocks_that_are_not_there_are_skipped():
             t = int(c.idx[0, 0, j])
             there = 0 <= t < c.n and t // 16 != 7 and j // 16 != 2
             assert (y[0, 0, j] == (x[0, 0, t] if there else 0)).all(), j
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("pool", [1, 5])
+def test_tokens_that_are_always_kept_come_before_infinite_masses(pool):
+    n = 64
+    ctx = sk.Context(sk.make_params(64, 1, 1, 16, 4, sk.BF16, 1, n, 8))
+    ctx.set_forced_tokens(0, 3)
+    mass = torch.ones((1, 1, n), device="cuda")
+    mass[0, 0, :40] = math.inf
+    scores, idx, count = torch.empty_like(mass), torch.full((1, 1, 8), -7, dtype=torch.int32, device="cuda"), harness.i32([[0]])
+    ctx.evict_select(mass, harness.i32([n]), harness.i32([5]), 1, scores, idx, count, pool=pool)
+    assert idx[0, 0].tolist() == [0, 1, 61, 62, 63, -1, -1, -1] and count.item() == 5
 
 
 @pytest.mark.gpu
