@@ -4,7 +4,9 @@
  * hand-written HIP.
  *
  * Call order for one attention layer (the paper's three stages):
- *   prefill : socket_hash_keys over all cached keys            (Alg. 1)
+ *   prefill : socket_attend_rows  attention of the prompt      (Eq. 1)
+ *             socket_hash_keys over all cached keys            (Alg. 1)
+ *   where the cache is bounded: socket_key_mass over the run, socket_evict_select, socket_evict_rows
  *   decode  : socket_hash_keys over the one appended key       (Alg. 1)
  *             socket_score        soft-hash q, score every key (Alg. 2 + Alg. 5 / Eq. 3)
  *             socket_topk_select  keep the k best tokens       (Alg. 3, TopK step)
@@ -357,7 +359,7 @@ int socket_decode_step(socket_ctx *ctx, const void *q, const void *K, const void
  * Positions are those of the cache as it stands: after an eviction, of the tokens that were kept.
  */
 typedef struct socket_attn_mods {
-    float softcap;             /* 0: scores are not capped */
+    float softcap;             /* 0: scores are not capped; else 1e-30 to 1e30, and scale / softcap finite */
     int32_t window;            /* a row sees itself and the window - 1 keys before it; 0: all of them */
     const float *slopes;       /* [Hq] bias by distance, or NULL */
     const int32_t *prefix_len; /* [B] the first tokens that every row sees, or NULL: causal throughout */
@@ -369,14 +371,14 @@ typedef struct socket_attn_mods {
  * prompt or all of it.  The caller has written K and V of the run's tokens, positions
  * row_begin[b] .. row_begin[b] + row_count[b] - 1 of a sequence that is then
  * row_begin[b] + row_count[b] tokens long (max_rows, on the host, bounds every row_count[b]; a run
- * that leaves [0, max_n) is cut to it).  For each row i and query head
+ * that goes past max_n is cut to it, one that begins outside [0, max_n) is empty).  For each row i and query head
  *     out = sum_j softmax(s)_j v_j,   lse = log sum_j exp(s_j)        over the keys the row sees.
  * q and out: [B, max_rows, Hq, d], out of type out_dtype; lse: float32 [B, max_rows, Hq] or NULL.
  * Rows behind row_count[b] are left as they were.  A row that sees no key gives zeros and
  * lse = -inf, and so does one whose scores all are -inf.  Keys and values that a row does not see
  * never count, infinities and NaN included.  q, K, V and out have to be aligned to 16 bytes.
  * bf16 caches: fp32 sums; where out is bf16 and max_rows Hq/Hkv is above 32, the softmax weights are
- * rounded to bf16 once.
+ * rounded to bf16 once.  scale lies within +-1e30.
  * row_begin, row_count: device int32 [batch].
  */
 int socket_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void *V, const int32_t *block_table,
@@ -391,7 +393,7 @@ int socket_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void
  * over the run's rows i that see j (only the last last_rows of them unless that is 0) and the
  * query heads g of KV head h.  Tokens of the run itself (j >= row_begin[b]) start from 0, whatever
  * mass held, and decay = 0 starts all of them from 0; tokens behind the sequence are left as they
- * were.  Summed in fp32 in a fixed order: the same masses bit for bit on every run.  q and K have
+ * were, and all of a sequence whose run is empty.  Summed in fp32 in a fixed order: the same masses bit for bit on every run.  q and K have
  * to be aligned to 16 bytes.
  * mass: device float32 [B, Hkv, max_n] in logical token order, for paged caches too.
  */
@@ -405,7 +407,8 @@ int socket_key_mass(socket_ctx *ctx, const void *q, const void *K, const float *
  * masses, each taken as the largest of the `pool` masses around it (odd, at most 255; 1: its own),
  * ties to the smaller position.  The tokens that socket_set_forced_tokens names are always kept
  * first, and tokens whose block is absent never; a mass that is NaN or -inf ranks below all
- * others, but its token can be kept, so that every head keeps the same number.  Writes the ranking into
+ * others, but its token can be kept, so that every head keeps the same number; +inf counts as the
+ * largest finite mass.  Writes the ranking into
  * scores ([B, Hkv, max_n] float32, not the array of masses), then idx and n_selected as
  * socket_topk_select does.  Like that call it discards a pending socket_score_keys_binned.
  * mass and scores have to be aligned to 16 bytes.

@@ -36,7 +36,7 @@ inline RowMods row_mods(float scale, const socket_attn_mods *m) {
 }
 
 // A run of rows: token positions begin .. begin + count - 1 of a sequence that is begin + count
-// long.  One that leaves [0, max_n) is cut to it.
+// long.  One that goes past max_n is cut to it, one that begins outside [0, max_n) is empty.
 struct RowRun {
     int begin, count;
     __device__ __forceinline__ RowRun(const int32_t *row_begin, const int32_t *row_count, int b, int max_rows, int max_n) {

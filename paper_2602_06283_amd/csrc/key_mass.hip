@@ -6,6 +6,11 @@
 // lane has one query (one lse, one span of keys) and a few keys, whose sums it keeps in registers;
 // the queries of a tile are added up once, at the end, in a fixed order.  No atomics: the same
 // masses bit for bit on every run.
+//
+// Bounds and figures: many queries by the matrix units and, as much, by the softmax's vector work, which no second
+// product shares: 4096 rows of 32 heads, d = 128, 118 us = 0.58 PFLOP/s, with a cap 160; fp32, 8 heads, 214 us =
+// 0.080 (a large product reaches 1.19, and 0.135 in fp32).  One token by memory: 16 ragged paged sequences up to
+// 32768 keys 145 us = 4.8 TB/s, what a large copy reaches.
 #include "attend_device.h"
 
 namespace sk {

@@ -391,8 +391,12 @@ int socket_dense_decode(socket_ctx *ctx, const void *q, const void *K, const voi
 
 static bool finite_f(float x) { return x == x && x <= 3.4e38f && x >= -3.4e38f; }
 
-static bool mods_ok(const socket_attn_mods *m) {
-    return !m || (finite_f(m->softcap) && m->softcap >= 0.0f && m->window >= 0);
+// scale, cap and their quotient as the kernels take them: far from where fp32 overflows, or loses bits
+static bool scores_ok(float scale, const socket_attn_mods *m) {
+    if (!finite_f(scale) || scale > 1e30f || scale < -1e30f) return false;
+    if (!m) return true;
+    if (m->softcap != 0.0f && !(m->softcap >= 1e-30f && m->softcap <= 1e30f)) return false;
+    return m->window >= 0 && (m->softcap == 0.0f || finite_f(scale / m->softcap));
 }
 
 // rows of q, K, V and what is written beside them are read and written 16 bytes at a time
@@ -408,7 +412,7 @@ int socket_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void
                        void *stream) {
     if (!ctx || !q || !K || !V || !row_begin || !row_count || !out) return SOCKET_EINVAL;
     if (!batch_ok(ctx, batch) || !paging_ok(ctx, block_table)) return SOCKET_EINVAL;
-    if (max_rows < 0 || max_rows > ctx->g.max_n || !finite_f(scale) || !mods_ok(mods)) return SOCKET_EINVAL;
+    if (max_rows < 0 || max_rows > ctx->g.max_n || !scores_ok(scale, mods)) return SOCKET_EINVAL;
     if (out_dtype != SOCKET_BF16 && out_dtype != SOCKET_F32) return SOCKET_EINVAL;
     if (!aligned16({q, K, V, out})) return SOCKET_EINVAL;
     if (max_rows == 0) return SOCKET_OK;
@@ -422,7 +426,7 @@ int socket_key_mass(socket_ctx *ctx, const void *q, const void *K, const float *
                     void *stream) {
     if (!ctx || !q || !K || !lse || !row_begin || !row_count || !mass) return SOCKET_EINVAL;
     if (!batch_ok(ctx, batch) || !paging_ok(ctx, block_table)) return SOCKET_EINVAL;
-    if (max_rows < 0 || max_rows > ctx->g.max_n || !finite_f(scale) || !mods_ok(mods)) return SOCKET_EINVAL;
+    if (max_rows < 0 || max_rows > ctx->g.max_n || !scores_ok(scale, mods)) return SOCKET_EINVAL;
     if (!finite_f(decay) || decay < 0.0f || last_rows < 0 || !aligned16({q, K})) return SOCKET_EINVAL;
     if (max_rows == 0) return SOCKET_OK;
     return launch_key_mass(ctx, q, K, lse, block_table, row_begin, row_count, batch, max_rows, scale, mods, decay,

@@ -489,6 +489,46 @@ def test_refusals():
                                   run.dbegin.data_ptr(), run.dcount.data_ptr(), 1, 4, 1.0, None, 5, out.data_ptr(), None, None) == sk.EINVAL
 
 
+@pytest.mark.gpu
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("mods", [dict(), dict(window=300, bias=True), dict(softcap=20.0, prefix=[500, 2, 0], docs=[130, 700])])
+def test_whole_prompts_split_over_keys_and_queries(mods, f32, d):
+    run = Run(94 + d, [0, 100, 0], [1100, 3, 0], G=1, d=d, f32=f32, **mods).device()
+    out, lse = run.attend(True)
+    run.check(out, lse)
+    before = torch.rand((3, run.Hkv, run.n), generator=torch.Generator().manual_seed(7)).double().float().double()
+    want, tol = run.masses(before, 0.5, 0, lse.cpu())
+    mass = before.float().cuda()
+    run.ctx.key_mass(run.dq, run.dK, lse, run.dbegin, run.dcount, 3, run.R, run.scale, mass, decay=0.5, **run.mods)
+    assert float(((mass.cpu().double() - want).abs() - tol).max()) <= 0
+    again = before.float().cuda()
+    run.ctx.key_mass(run.dq, run.dK, lse, run.dbegin, run.dcount, 3, run.R, run.scale, again, decay=0.5, **run.mods)
+    assert torch.equal(mass, again)
+
+
+@pytest.mark.gpu
+def test_caps_and_scales_where_fp32_ends():
+    run = Run(92, [40], [4]).device()
+    out, lse = run.attend(True)
+    mass = torch.zeros((1, run.Hkv, run.n), device="cuda")
+    for scale, cap in ((1e31, 0.0), (-1e31, 0.0), (1.0, 1e-39), (1.0, 1e38), (1e20, 1e-20)):
+        for call in (lambda: run.ctx.attend_rows(run.dq, run.dK, run.dV, run.dbegin, run.dcount, 1, 4, scale, out, softcap=cap),
+                     lambda: run.ctx.key_mass(run.dq, run.dK, lse, run.dbegin, run.dcount, 1, 4, scale, mass, softcap=cap)):
+            with pytest.raises(sk.SocketError) as e:
+                call()
+            assert e.value.code == sk.EINVAL, (scale, cap)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [4, 90])
+@pytest.mark.parametrize("f32", [False, True])
+@pytest.mark.parametrize("cap", [1e30, 1e-30])           # as good as none; every score is the cap or its negative
+def test_the_largest_and_the_smallest_cap(cap, f32, rows):
+    run = Run(93, [40], [rows], f32=f32, softcap=cap).device()
+    run.check(*run.attend(True))
+
+
 def test_null_arguments_are_refused_without_a_gpu():
     lib = sk.lib()
     assert lib.socket_attend_rows(None, None, None, None, None, None, None, 1, 1, 1.0, None, 1, None, None, None) == sk.EINVAL
