@@ -22,7 +22,7 @@
 // Bounds and figures (a large copy reaches 4.85 TB/s here, a large matrix product 1.19 PFLOP/s in bf16
 // and 0.135 in fp32, all under the card's power limit).  Prompts and chunks are bound by the matrix units and the
 // softmax's vector work beside them: 8192 rows of 32 heads, d = 128, 575 to 618 us on several cards = 0.89 to
-// 0.96 PFLOP/s; 4096 rows behind 28672, capped, 2510 us = 0.82 (a cap is six more operations a logit); 4096 fp32
+// 0.96 PFLOP/s; 4096 rows behind 28672, capped, 2510 us = 0.82 (a cap is seven more operations a logit); 4096 fp32
 // rows of 8 heads 330 us = 0.104.  One token is bound by memory: 131072 keys of 8 heads 96 us = 5.6 TB/s, 16 ragged
 // paged sequences 266 us = 5.05 TB/s.  4096 keys of one head, fp32, 11.7 us: the latency of two launches.
 //
@@ -1040,8 +1040,8 @@ int launch_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void
     const int64_t room = ctx->partial_floats / ((int64_t)batch * max_rows * g.Hq * (g.d + 2));   // splits whose results fit
     const bool f32 = g.kv_dtype == SOCKET_F32;
     if ((int64_t)max_rows * g.G <= 32) {
-        // One wavefront a split, at least a tile of keys each: with 16 and more of them to a compute unit the last
-        // ones to finish are a small part.
+        // One wavefront a split, 32 keys each at least (64: 4096 fp32 keys of one head 14.5 us, not 11.6; 131072 of 8
+        // heads the same): with 16 and more of them to a compute unit the last ones to finish are a small part.
         // More than 16 queries are two column blocks of a wavefront, at d = 256 (whose registers do not hold
         // two: 8 rows of 4 heads behind 32000 151 us) of two wavefronts.
         const bool two = max_rows * g.G > 16, wide = two && g.d < 256;
