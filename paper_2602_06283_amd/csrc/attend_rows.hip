@@ -161,15 +161,19 @@ template <int D, int PX> struct ValueStages<uint16_t, D, PX> {
     // rows 16 ks + 4 hf + 0..3 and + 8 of sub-tile u: a sixteenth of the wavefront reads four rows of 16 channels,
     // transposed
     static __device__ __forceinline__ Part read(const char *v, int stage, int lane) {
-        const int u = stage / (D / 32), ks = stage / (D / 64) % 2, cb0 = stage % (D / 64) * 2, hf = lane >> 5;
-        const int row = 32 * u + 16 * ks + 4 * hf + ((lane & 15) >> 2);
-        const int c0 = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), in = (lane & 1) * 8;
+        const int u = stage / (D / 32), ks = stage / (D / 64) % 2, cb0 = stage % (D / 64) * 2;
+        // v_piece with the lane's part apart, which is one of four (two at d = 64): an address of its own for every
+        // read took registers that the kernel lacked
+        const int r = (lane & 15) >> 2, turn = Tile::CPR == 8 ? r >> 1 : r, last = Tile::CPR == 8 ? 1 : 3;
+        const int at = (4 * (lane >> 5) + r) * Tile::ROWB + (((lane >> 4) & 1) * 2 + ((lane & 3) >> 1)) * 16 + (lane & 1) * 8;
         Part part;
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
+            const int cb = cb0 + y;
+            const char *from = v + at + 64 * ((cb & last) ^ turn) + ((32 * u + 16 * ks) * Tile::ROWB + 256 * (cb / 4));
             union { shortx4_t h[2]; u32x4_t v; } f;
-            f.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(v + Tile::v_piece(row, c0 + 4 * (cb0 + y)) * 16 + in));
-            f.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(v + Tile::v_piece(row + 8, c0 + 4 * (cb0 + y)) * 16 + in));
+            f.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)from);
+            f.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_shortx4_t *)(from + 8 * Tile::ROWB));
             part.v[y] = f.v;
         }
         return part;
@@ -305,6 +309,9 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(kR
             s_rows[x] = (int)a.map.row(b, h, t);     // (rows are numbered in 31 bits; -1: no block)
         }
     };
+    int row[LOADS];                                  // paged: where the rows of K begin that were loaded last; V's of that tile are next
+#pragma unroll
+    for (int p = 0; p < LOADS; ++p) row[p] = 0;
     auto load_rows = [&](int tile, const char *head, uint32_t byte, char *to, auto is_v) __attribute__((always_inline)) {
         constexpr bool VALUES = decltype(is_v)::value;
         const int t0 = base + tile * KT;
@@ -315,16 +322,17 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(kR
             for (int p = 0; p < LOADS; ++p)
                 lds_fill(from + p * RPL * Tile::ROWB + (ONE_TURN ? byte : byte_of(p, VALUES)), to + (p * kRowsThreads + wave * 64) * 16);
         } else {
-            int row[LOADS];
-            if (paged) {
+            if (paged && !VALUES) {
 #pragma unroll
                 for (int p = 0; p < LOADS; ++p) row[p] = s_rows[(tile - looked_up) * NG + (p * RPL + w_row) / 16];
+#pragma unroll
+                for (int p = 0; p < LOADS; ++p) row[p] = max(__builtin_amdgcn_readfirstlane(row[p]), 0);
             }
 #pragma unroll
             for (int p = 0; p < LOADS; ++p) {
                 const int in16 = (p * RPL + w_row) % 16;          // the wavefront's first row in its sixteen
                 const int first = min(t0 + p * RPL + w_row - in16, k_hi & ~15);
-                const int start = paged ? max(__builtin_amdgcn_readfirstlane(row[p]), 0) : first - base;
+                const int start = paged ? row[p] : first - base;
                 const char *from = head + (int64_t)start * Tile::ROWB;
                 // (rows behind the last key read it again)
                 const int in = min(in16 + l_row, k_hi - first);
@@ -355,7 +363,8 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(kR
     constexpr bool SERIAL = sizeof(T) == 4;
     auto read_k = [&](const char *kt, int ks, u32x4_t (&f)[NU]) __attribute__((always_inline)) {
 #pragma unroll
-        for (int u = 0; u < NU; ++u) f[u] = *(const u32x4_t *)(kt + Tile::k_piece(32 * u + (lane & 31), 2 * ks + hf) * 16);
+        for (int u = 0; u < NU; ++u)                  // (k_piece of row 32 u + lane % 32)
+            f[u] = *(const u32x4_t *)(kt + Tile::k_piece(lane & 31, 2 * ks + hf) * 16 + 32 * u * Tile::ROWB);
     };
     auto products = [&](const char *kt, floatx16_t (&s)[NU]) __attribute__((always_inline)) {
 #pragma unroll
