@@ -21,9 +21,9 @@
 //
 // Bounds and figures (a large copy reaches 4.85 TB/s here, a large matrix product 1.19 PFLOP/s in bf16
 // and 0.135 in fp32, all under the card's power limit).  Prompts and chunks are bound by the matrix units and the
-// softmax's vector work beside them: 8192 rows of 32 heads, d = 128, 575 to 618 us on several cards = 0.89 to
-// 0.96 PFLOP/s; 4096 rows behind 28672, capped, 2510 us = 0.82 (a cap is seven more operations a logit); 4096 fp32
-// rows of 8 heads 330 us = 0.104.  One token is bound by memory: 131072 keys of 8 heads 96 us = 5.6 TB/s, 16 ragged
+// softmax's vector work beside them: 8192 rows of 32 heads, d = 128, 547 to 583 us on several cards = 0.94 to
+// 1.0 PFLOP/s; 4096 rows behind 28672, capped, 2370 us = 0.87 (a cap is seven more operations a logit); 4096 fp32
+// rows of 8 heads 321 us = 0.107.  One token is bound by memory: 131072 keys of 8 heads 96 us = 5.6 TB/s, 16 ragged
 // paged sequences 266 us = 5.05 TB/s.  4096 keys of one head, fp32, 11.7 us: the latency of two launches.
 //
 // Values at masked keys never count, whatever they are: a masked weight is 0, but 0 times an
@@ -424,7 +424,7 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(kR
     };
     // One tile, whose logits are there.  The exponentials run beside the products of the next tile's keys, its
     // values beside the next tile's logits; the tile after that is on its way.  In stages of a few matrix instructions,
-    // whose operands are read from LDS a stage before (the compiler's own order reads each right before its
+    // whose operands are read from LDS a stage or two before (the compiler's own order reads each right before its
     // use, and every matrix instruction waits for LDS) and the vector work of the softmax shared out among them.
     auto sees = [&](int tile) __attribute__((always_inline)) {
         const int t0 = base + tile * KT;
@@ -433,7 +433,9 @@ __global__ __launch_bounds__(kRowsThreads) __attribute__((amdgpu_waves_per_eu(kR
     bool seen = true;                                // whether the wavefront sees the tile at hand
     auto tile_step = [&](int tile, floatx16_t (&s)[NU], const char *k_next, const char *v_now, char *k_to, char *v_to) __attribute__((always_inline)) {
         using Values = ValueStages<T, D, PX>;
-        constexpr int AHEAD = 1, RING = AHEAD + 1;
+        // (stages that operands are read ahead; 4096 rows, 16 heads, d = 256: 223 us with one, 211 with two; d = 128, 8192
+        // rows 551 and 547; capped logits lack the registers, 212 and 220 with a bias)
+        constexpr int AHEAD = CAP ? 1 : 2, RING = AHEAD + 1;
         u32x4_t fk[RING][NU];
         typename Values::Part fv[RING];
         Values values;
