@@ -1074,12 +1074,15 @@ int launch_attend_rows(socket_ctx *ctx, const void *q, const void *K, const void
         // out (4096 fp32 rows of 8 heads 455 -> 340 us, 8192 bf16 rows of 8 heads 221 -> 200; but 2048 rows behind
         // 16384 179 -> 197; at d = 256 four to a compute unit: 2048 fp32 rows of 8 heads 195 -> 230).
         // A split's products have to be worth the results it leaves: 512 keys and more in bf16 (256: 512 prompt rows
-        // 23 us with the launch that joins them, 18 without); in fp32 they take longer the wider the heads (512 at
+        // of 32 heads 23 us with the launch that joins them, 17 without), 256 or 128 where a tile of queries or two is
+        // all there is and the chain of a split's tiles is what the call waits for (34 rows behind 1633, 16 workgroups,
+        // 18 us with 512, 14 with 128; 167 rows of 16 heads behind 2436, 24 workgroups, 23 with 512, 22 with 256, 29
+        // with 128); in fp32 they take longer the wider the heads (512 at
         // d = 64: 256 there 33 -> 42 us for 2011 rows; 256 at d = 128: 1024 rows 97 -> 59; 128 at d = 256: 300 rows
         // 54 -> 46).
         a.n_tiles = (int)(((int64_t)max_rows * g.G + kRowsQueries - 1) / kRowsQueries);
         const int64_t wgs = (int64_t)a.BH * a.n_tiles;
-        const int wanted = (2 * (int64_t)max_rows >= g.max_n ? 1024 : 512) / (g.d == 256 ? 2 : 1), least = f32 ? 32768 / g.d : 512;
+        const int wanted = (2 * (int64_t)max_rows >= g.max_n ? 1024 : 512) / (g.d == 256 ? 2 : 1), least = f32 ? 32768 / g.d : wgs <= 16 ? 128 : wgs <= 64 ? 256 : 512;
         a.n_split = pick_splits(wanted / wgs, (g.max_n + least - 1) / least, room);
         const int64_t grid = wgs * a.n_split;
         if (grid * kRowsThreads >= (int64_t)1 << 32) return SOCKET_EUNSUPPORTED;
